@@ -393,6 +393,112 @@ VECTOR_API int vector_decode_step_rope(const vector_cache* cache, const vector_r
                             const void* v_new, float scale, void* out, int32_t flags, void* ws, size_t ws_bytes,
                             void* stream);
 
+/* ---- blocks of a paged cache ---------------------------------------------- */
+
+/* Block tables and slot maps from request lengths that lie on the GPU: what a paged cache (the retained segments of
+ * vector_cache and vector_cache_fp4) needs for the next tokens of a batch, without the lengths coming to the host.
+ * Request b holds blocks for len_held[b] rows per KV head and asks for len[b]; with R = block_rows it needs
+ * n_b = ceil(len[b] / R) - ceil(len_held[b] / R) more blocks per KV head.  Requests are admitted in order while the free
+ * blocks last: b is admitted if n_b = 0, or if n_kv_heads * (n_0 + .. + n_b) <= n_free; and, where slots are asked for
+ * and it has new tokens, if they all fit the slot map; never if len[b] is more than a row of the table has blocks for
+ * (it then counts as needing none).  A length below zero counts as zero, len[b] below len_held[b] as len_held[b].
+ *   block_table  device [batch, n_kv_heads, blocks_per_seq]: an admitted request's new blocks, KV head after KV head, are the next
+ *                ones of free_blocks.  With len_held, only the entries of new blocks are written; without (all
+ *                requests are new), every entry is, those without a block with 0.
+ *   len_live     device [batch]: len[b] of an admitted request (len_held[b] if that is more), len_held[b] of another (0 without
+ *                len_held).  What vector_cache calls len_retain once the new rows are stored.  Not the memory of len or len_held.
+ *   slots        NULL (or n_slots 0): none are asked for; or device [n_kv_heads, n_slots]: the rows of the pools (block id * R + row in the block) of the
+ *                new tokens, request after request (tokens len_held[b] .. len[b] - 1); -1 for tokens of requests that are not
+ *                admitted and for columns behind the last token.  0 <= n_slots < 2^31 - 1.
+ *   counts       device [VECTOR_BLOCK_COUNTS]: blocks taken from the front of free_blocks, blocks that all requests together need,
+ *                new tokens of all requests (both stop at 2^31 - 1)
+ * VECTOR_ERR_SHAPE: more than 4096 requests, or a table of 2^31 entries or more. */
+typedef struct {
+  int32_t batch, n_kv_heads;
+  int32_t block_rows;            /* R: a power of two, at least 16                           */
+  int32_t blocks_per_seq;        /* entries of a row of the table                            */
+  int32_t n_free;
+  int32_t reserved;
+  const int32_t* len_held;       /* device [batch], or NULL: no request holds blocks yet     */
+  const int32_t* len;            /* device [batch]                                           */
+  const int32_t* free_blocks;    /* device [n_free]: ids of free blocks; NULL: 0, 1, 2, ..   */
+} vector_blocks;
+#define VECTOR_BLOCK_COUNTS 3
+VECTOR_API int vector_block_tables(const vector_blocks* blocks, int32_t* block_table, int32_t* len_live, int64_t* slots,
+                                   int64_t n_slots, int32_t* counts, void* stream);
+
+/* ---- caches held in 4 bits -------------------------------------------------- */
+
+/* A row of head_dim elements in 4 bits is head_dim / 2 bytes of codes and, in an array of its own, head_dim / 32 bytes of scales.
+ * A code is an E2M1 number (magnitudes 0, 0.5, 1, 1.5, 2, 3, 4, 6; bit 3 the sign), element 2 i in the low half of byte i.  A
+ * scale byte belongs to 32 elements and stands for 2^(byte - 127); 255 stands for NaN (microscaled 4-bit floating point).
+ * Rows are rounded so: the scale of a block is the smallest power of two of which 7 is no less than the block's largest
+ * magnitude, 2^-126 at least and 2^125 at most; every element goes to the nearest code, ties to the even one.  So no element (up to
+ * 7 * 2^125 = 2.98e38) is off by more than one scale, and every value is finite in fp32 and bf16; a block with an infinite or NaN
+ * element is NaN.
+ * Code and scale arrays are device memory, 16-byte aligned. */
+#define VECTOR_FP4_BLOCK 32
+
+/* vector_compact into 4 bits: the packed cache that vector_decode_attn_fp4 reads, from the routing's lists.
+ *   k_ret, v_ret    codes  device [Hkv, cap_retain, d / 2],  scales device [Hkv, cap_retain, d / 32]
+ *   k_apx           codes  device [Hkv, n_approx, d / 2],    scales device [Hkv, n_approx, d / 32]
+ * Rows beyond n_retain are left untouched.  Other arguments and errors as there.  An index outside 0 .. seq_len - 1
+ * leaves its row untouched. */
+VECTOR_API int vector_compact_fp4(const vector_shape* shape, const void* k, const void* v, const int32_t* idx_retain, const int32_t* idx_approx,
+                       int32_t n_retain, int32_t n_approx, uint8_t* k_ret, uint8_t* k_ret_scale, uint8_t* v_ret,
+                       uint8_t* v_ret_scale, uint8_t* k_apx, uint8_t* k_apx_scale, int32_t cap_retain, void* stream);
+
+/* Rows into pools of rows in 4 bits by slots (those of vector_block_tables, or any others): row t of KV head h of k (and of v,
+ * which may be NULL with its pool) goes to row slots[h * seq_len + t] of the pools, which have pool_rows rows.  A row whose slot is
+ * negative or not below pool_rows goes nowhere.  Slots must differ.  k, v: [Hkv, seq_len, d] with the shape's strides and dtype;
+ * slots: device [Hkv, seq_len].  seq_len is not limited here. */
+VECTOR_API int vector_store_fp4(const vector_shape* shape, const void* k, const void* v, const int64_t* slots, int64_t pool_rows,
+                     uint8_t* k_pool, uint8_t* k_pool_scale, uint8_t* v_pool, uint8_t* v_pool_scale, void* stream);
+
+/* The values of rows in 4 bits: out[r] (device [n_rows, head_dim] of dtype) is row slots[r] of an array of pool_rows rows, row r where
+ * slots is NULL; zeros where there is no such row.  The values of fp32 are exact; those of bf16 too. */
+VECTOR_API int vector_load_fp4(int64_t n_rows, int32_t head_dim, int32_t dtype, const uint8_t* codes, const uint8_t* scales,
+                    int64_t pool_rows, const int64_t* slots, void* out, void* stream);
+
+/* vector_cache with its rows in 4 bits.  Everything is laid out as there, in rows of codes and rows of scales: k_ret, k_ret_scale
+ * [batch, Hkv, cap_retain, ..] and so on; dtype is that of q, W, out and the step's token. */
+typedef struct {
+  int32_t batch, n_q_heads, n_kv_heads, head_dim;
+  int32_t dtype;
+  int32_t cap_retain, n_approx;
+  int32_t w_shared;
+  const int32_t* len_retain;
+  const uint8_t* k_ret;
+  const uint8_t* k_ret_scale;
+  const uint8_t* v_ret;
+  const uint8_t* v_ret_scale;
+  const uint8_t* k_apx;
+  const uint8_t* k_apx_scale;
+  const void* W;
+  const int32_t* cap_retain_seq;
+  const int32_t* n_approx_seq;
+  const int64_t* ret_row_start;
+  const int64_t* apx_row_start;
+  const int32_t* ret_block_table;
+  int32_t ret_block_rows;
+  int32_t ret_blocks_per_seq;
+  int32_t n_blocks;              /* paged: blocks of the pools.  Rows of a block whose id is not in 0 .. n_blocks - 1 are no rows: they
+                                    take no part, and a step's token in one is attended but not stored */
+  int32_t reserved;
+} vector_cache_fp4;
+
+/* vector_decode_attn and vector_decode_step over a cache in 4 bits, rope NULL, or vector_decode_attn_rope and
+ * vector_decode_step_rope.  Same arguments, flags (VECTOR_DECODE_OUT_F32), outputs and errors.  The step rounds the new token to 4 bits
+ * and attends to it as it lies in the cache from then on, so that it gives what storing the row and
+ * vector_decode_attn_fp4 would.  The products run on the matrix cores in bf16 with fp32 sums; bf16: weights to 2^-16 relative at least;
+ * fp32: query and weights with all their bits.  VECTOR_DECODE_LITERAL: VECTOR_ERR_DTYPE.
+ * ws: vector_decode_fp4_workspace_bytes(cache) bytes (0 for a shape that is refused), 256-byte aligned. */
+VECTOR_API size_t vector_decode_fp4_workspace_bytes(const vector_cache_fp4* cache);
+VECTOR_API int vector_decode_attn_fp4(const vector_cache_fp4* cache, const vector_rope* rope, const void* q, float scale, void* out,
+                           int32_t flags, void* ws, size_t ws_bytes, void* stream);
+VECTOR_API int vector_decode_step_fp4(const vector_cache_fp4* cache, const vector_rope* rope, const void* q, const void* k_new,
+                           const void* v_new, float scale, void* out, int32_t flags, void* ws, size_t ws_bytes, void* stream);
+
 /* ---- calibration of the value map ---------------------------------------- */
 
 /* Section 3.1: the least-squares map from keys to values, per KV head and without intercept,

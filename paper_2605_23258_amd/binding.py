@@ -35,6 +35,8 @@ EXPORTS = (
     "vector_distortion_workspace_bytes", "vector_distortion",
     "vector_r2_workspace_bytes", "vector_r2",
     "vector_score_key_diversity_workspace_bytes", "vector_score_key_diversity",
+    "vector_block_tables", "vector_compact_fp4", "vector_store_fp4", "vector_load_fp4",
+    "vector_decode_fp4_workspace_bytes", "vector_decode_attn_fp4", "vector_decode_step_fp4",
 )
 
 
@@ -98,6 +100,32 @@ def make_batch(seq_len, n_pool, n_approx, cap_retain):
     arrs = [(C.c_int32 * len(seq_len))(*[int(x) for x in a]) for a in (seq_len, n_pool, n_approx, cap_retain)]
     assert len({len(a) for a in arrs}) == 1
     return Batch(len(seq_len), *[C.cast(a, C.POINTER(C.c_int32)) for a in arrs]), arrs
+
+
+class Blocks(C.Structure):
+    """vector_blocks: requests that ask for blocks of a paged cache."""
+    _fields_ = [("batch", C.c_int32), ("n_kv_heads", C.c_int32), ("block_rows", C.c_int32), ("blocks_per_seq", C.c_int32),
+                ("n_free", C.c_int32), ("reserved", C.c_int32), ("len_held", C.c_void_p), ("len", C.c_void_p), ("free_blocks", C.c_void_p)]
+
+
+def make_blocks(length, n_kv_heads: int, block_rows: int, blocks_per_seq: int, free, held=None) -> Blocks:
+    """Blocks from device int32 tensors: lengths asked for, ids of free blocks, and the lengths that the requests hold blocks for (None:
+    all requests are new).  The tensors have to outlive it."""
+    return Blocks(batch=length.numel(), n_kv_heads=n_kv_heads, block_rows=block_rows, blocks_per_seq=blocks_per_seq, n_free=free.numel(),
+                  len_held=_ptr(held), len=_ptr(length), free_blocks=_ptr(free))
+
+
+class CacheFp4(C.Structure):
+    """vector_cache_fp4: a cache held in 4 bits, rows of codes and rows of scales."""
+    _fields_ = [
+        ("batch", C.c_int32), ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+        ("dtype", C.c_int32), ("cap_retain", C.c_int32), ("n_approx", C.c_int32), ("w_shared", C.c_int32),
+        ("len_retain", C.c_void_p), ("k_ret", C.c_void_p), ("k_ret_scale", C.c_void_p), ("v_ret", C.c_void_p), ("v_ret_scale", C.c_void_p),
+        ("k_apx", C.c_void_p), ("k_apx_scale", C.c_void_p), ("W", C.c_void_p),
+        ("cap_retain_seq", C.c_void_p), ("n_approx_seq", C.c_void_p), ("ret_row_start", C.c_void_p), ("apx_row_start", C.c_void_p),
+        ("ret_block_table", C.c_void_p), ("ret_block_rows", C.c_int32), ("ret_blocks_per_seq", C.c_int32),
+        ("n_blocks", C.c_int32), ("reserved", C.c_int32),
+    ]
 
 
 _lib = None
@@ -171,6 +199,14 @@ def lib() -> C.CDLL:
         L.vector_residual_rope.argtypes = [C.POINTER(Shape), vp, vp, vp, C.POINTER(Rope), vp, vp, sz, vp]
         L.vector_score_residual_rope.argtypes = [C.POINTER(Shape), vp, vp, vp, vp, C.POINTER(Rope), vp, vp, vp, sz, vp]
         L.vector_decode_attn_rope.argtypes = [C.POINTER(Cache), C.POINTER(Rope), vp, C.c_float, vp, i32, vp, sz, vp]
+        L.vector_block_tables.argtypes = [C.POINTER(Blocks), vp, vp, vp, C.c_int64, vp, vp]
+        L.vector_compact_fp4.argtypes = [C.POINTER(Shape), vp, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp, vp, i32, vp]
+        L.vector_store_fp4.argtypes = [C.POINTER(Shape), vp, vp, vp, C.c_int64, vp, vp, vp, vp, vp]
+        L.vector_load_fp4.argtypes = [C.c_int64, i32, i32, vp, vp, C.c_int64, vp, vp, vp]
+        L.vector_decode_fp4_workspace_bytes.argtypes = [C.POINTER(CacheFp4)]
+        L.vector_decode_fp4_workspace_bytes.restype = sz
+        L.vector_decode_attn_fp4.argtypes = [C.POINTER(CacheFp4), C.POINTER(Rope), vp, C.c_float, vp, i32, vp, sz, vp]
+        L.vector_decode_step_fp4.argtypes = [C.POINTER(CacheFp4), C.POINTER(Rope), vp, vp, vp, C.c_float, vp, i32, vp, sz, vp]
         _lib = L
     return _lib
 
@@ -456,3 +492,42 @@ def vector_score_key_diversity_workspace_bytes(shape: Shape) -> int:
 def vector_score_key_diversity(shape: Shape, k, score, ws, stream=None) -> None:
     _check(lib().vector_score_key_diversity(C.byref(shape), _ptr(k), _ptr(score), _ptr(ws), _nbytes(ws), _stream(stream)),
            "vector_score_key_diversity")
+
+
+def vector_block_tables(blocks: Blocks, block_table, len_live, slots, counts, stream=None) -> None:
+    """Block table, live lengths and (slots not None: [n_kv_heads, n_slots]) slots of the new tokens of a batch of requests."""
+    _check(lib().vector_block_tables(C.byref(blocks), _ptr(block_table), _ptr(len_live), _ptr(slots),
+                                     0 if slots is None else int(slots.shape[-1]), _ptr(counts), _stream(stream)), "vector_block_tables")
+
+
+def vector_compact_fp4(shape: Shape, k, v, idx_retain, idx_approx, n_retain: int, n_approx: int, k_ret, k_ret_scale, v_ret, v_ret_scale,
+                       k_apx, k_apx_scale, cap_retain: int, stream=None) -> None:
+    _check(lib().vector_compact_fp4(C.byref(shape), _ptr(k), _ptr(v), _ptr(idx_retain), _ptr(idx_approx), n_retain, n_approx,
+                                    _ptr(k_ret), _ptr(k_ret_scale), _ptr(v_ret), _ptr(v_ret_scale), _ptr(k_apx), _ptr(k_apx_scale),
+                                    cap_retain, _stream(stream)), "vector_compact_fp4")
+
+
+def vector_store_fp4(shape: Shape, k, v, slots, pool_rows: int, k_pool, k_pool_scale, v_pool=None, v_pool_scale=None, stream=None) -> None:
+    _check(lib().vector_store_fp4(C.byref(shape), _ptr(k), _ptr(v), _ptr(slots), pool_rows, _ptr(k_pool), _ptr(k_pool_scale),
+                                  _ptr(v_pool), _ptr(v_pool_scale), _stream(stream)), "vector_store_fp4")
+
+
+def vector_load_fp4(n_rows: int, head_dim: int, dtype: int, codes, scales, pool_rows: int, slots, out, stream=None) -> None:
+    _check(lib().vector_load_fp4(n_rows, head_dim, dtype, _ptr(codes), _ptr(scales), pool_rows, _ptr(slots), _ptr(out),
+                                 _stream(stream)), "vector_load_fp4")
+
+
+def vector_decode_fp4_workspace_bytes(cache: CacheFp4) -> int:
+    return int(lib().vector_decode_fp4_workspace_bytes(C.byref(cache)))
+
+
+def vector_decode_attn_fp4(cache: CacheFp4, q, scale: float, out, ws, rope: Optional[Rope] = None, flags: int = 0, stream=None) -> None:
+    _check(lib().vector_decode_attn_fp4(C.byref(cache), None if rope is None else C.byref(rope), _ptr(q), float(scale), _ptr(out), flags,
+                                        _ptr(ws), _nbytes(ws), _stream(stream)), "vector_decode_attn_fp4")
+
+
+def vector_decode_step_fp4(cache: CacheFp4, q, k_new, v_new, scale: float, out, ws, rope: Optional[Rope] = None, flags: int = 0,
+                           stream=None) -> None:
+    """Decode attention over a cache in 4 bits with the step's own token rounded and appended (cache rows and len_retain are written)."""
+    _check(lib().vector_decode_step_fp4(C.byref(cache), None if rope is None else C.byref(rope), _ptr(q), _ptr(k_new), _ptr(v_new),
+                                        float(scale), _ptr(out), flags, _ptr(ws), _nbytes(ws), _stream(stream)), "vector_decode_step_fp4")

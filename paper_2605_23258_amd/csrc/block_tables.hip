@@ -1,0 +1,162 @@
+// Blocks of a paged cache for the requests of a batch, and the slots of their tokens, from lengths on the GPU (vector_block_tables).
+//
+// Which blocks a request gets follows from the requests before it: one running sum over the batch of the blocks they need
+// and one of their tokens.  There is one launch, without workspace: every workgroup makes both sums for itself (a batch of up to kMaxRequests lengths,
+// which lie in the L2 after the first workgroup's read) and then writes its part of the slots or of the table.  A second launch that
+// only read the sums would cost more than they do.  What is left is bound by the writes: 8 bytes per token and KV head.
+#include "common.hpp"
+#include "launch.hpp"
+
+namespace vec {
+
+namespace {
+
+constexpr int kThreads = 256, kWaves = kThreads / kWave;
+constexpr int kTokensPerGroup = 1024;        // slots a workgroup writes for every KV head
+constexpr int kPairsPerGroup = 8;            // (request, KV head) rows of the table a workgroup writes
+
+struct TableParams {
+  const int32_t *held, *len, *free_blocks;
+  int32_t *table, *live, *counts;
+  int64_t* slots;
+  int B, H, shift, per_seq, n_free, n_slots;
+  int slot_groups;                           // workgroups that write slots, those that write the table follow
+};
+
+// A request's lengths as they count: none below zero, and none below what it holds
+struct Request { int held, len; };
+__device__ __forceinline__ Request request(const TableParams& p, int b) {
+  const int held = p.held ? max(p.held[b], 0) : 0;
+  return {held, max(p.len[b], held)};
+}
+__device__ __forceinline__ int blocks_of(int rows, int shift) { return (int)(((int64_t)rows + (1 << shift) - 1) >> shift); }
+// blocks it asks for, for one KV head; a request longer than a row of the table asks for none, and is not admitted
+__device__ __forceinline__ bool too_long(const TableParams& p, const Request& r) { return blocks_of(r.len, p.shift) > p.per_seq; }
+__device__ __forceinline__ int wanted(const TableParams& p, const Request& r) {
+  return too_long(p, r) ? 0 : blocks_of(r.len, p.shift) - blocks_of(r.held, p.shift);
+}
+// blocks, tokens: of the requests up to this one
+__device__ __forceinline__ bool admitted(const TableParams& p, const Request& r, int blocks, int tokens) {
+  if (too_long(p, r)) return false;
+  return (wanted(p, r) == 0 || blocks <= p.n_free) && (!p.slots || r.len == r.held || tokens <= p.n_slots);
+}
+
+__device__ __forceinline__ int64_t wave_incl_scan64(int64_t x, int lane) {
+#pragma unroll
+  for (int o = 1; o < kWave; o <<= 1) {
+    const int64_t y = __shfl_up(x, o, kWave);
+    if (lane >= o) x += y;
+  }
+  return x;
+}
+
+__global__ __launch_bounds__(kThreads) void block_tables_kernel(TableParams p) {
+  extern __shared__ int sums[];              // [B + 1] blocks of one KV head up to a request times KV heads, [B + 1] tokens
+  __shared__ int64_t wave_blocks[kWaves], wave_tokens[kWaves];
+  int *blocks = sums, *tokens = sums + p.B + 1;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  int64_t base_blocks = 0, base_tokens = 0;
+  if (tid == 0) blocks[0] = tokens[0] = 0;
+  for (int b0 = 0; b0 < p.B; b0 += kThreads) {
+    const int b = b0 + tid;
+    const Request r = b < p.B ? request(p, b) : Request{0, 0};
+    int64_t nb = wave_incl_scan64((int64_t)wanted(p, r) * p.H, lane), nt = wave_incl_scan64((int64_t)r.len - r.held, lane);
+    if (lane == 63) { wave_blocks[wave] = nb; wave_tokens[wave] = nt; }
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      if (w < wave) { nb += wave_blocks[w]; nt += wave_tokens[w]; }
+    }
+    nb += base_blocks;
+    nt += base_tokens;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) { base_blocks += wave_blocks[w]; base_tokens += wave_tokens[w]; }
+    if (b < p.B) {
+      blocks[b + 1] = (int)nb;                                  // at most B * H * per_seq, which the host has checked
+      tokens[b + 1] = (int)min(nt, (int64_t)INT32_MAX);         // slots end before that
+    }
+    __syncthreads();
+  }
+
+  if ((int)blockIdx.x < p.slot_groups) {
+    // slots: a thread takes a token for all KV heads; neighbours are tokens of one request, mostly
+    const int t0 = blockIdx.x * kTokensPerGroup;
+    for (int t = t0 + tid; t < min(t0 + kTokensPerGroup, p.n_slots); t += kThreads) {
+      // the request b with tokens[b] <= t < tokens[b + 1]
+      int lo = 0, hi = p.B;                  // tokens[lo] <= t; hi == B or t < tokens[hi]
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (tokens[mid] <= t) lo = mid; else hi = mid;
+      }
+      const int b = lo;
+      const bool any = t < tokens[b + 1];    // behind the last token: no slot
+      const Request r = request(p, b);
+      const bool ok = any && admitted(p, r, blocks[b + 1], tokens[b + 1]);
+      const int pos = r.held + (t - tokens[b]), before = blocks_of(r.held, p.shift), n = wanted(p, r), at = pos >> p.shift;
+      for (int h = 0; h < p.H; ++h) {
+        int64_t slot = -1;
+        if (ok) {
+          // a new block comes from the free list, a block that the request holds from the table (this launch does not write these)
+          const int id = at >= before ? (p.free_blocks ? p.free_blocks[blocks[b] + h * n + at - before] : blocks[b] + h * n + at - before)
+                                      : p.table[((int64_t)b * p.H + h) * p.per_seq + at];
+          slot = ((int64_t)id << p.shift) + (pos & ((1 << p.shift) - 1));
+        }
+        p.slots[(int64_t)h * p.n_slots + t] = slot;
+      }
+    }
+    return;
+  }
+  const int group = blockIdx.x - p.slot_groups;
+  if (group == 0) {
+    for (int b = tid; b < p.B; b += kThreads) {
+      const Request r = request(p, b);
+      p.live[b] = admitted(p, r, blocks[b + 1], tokens[b + 1]) ? r.len : r.held;
+    }
+  }
+  if (group == 0 && wave == 0) {
+    // blocks taken: those of the admitted requests, which are the first ones that ask for any
+    int taken = 0;
+    for (int b = lane; b < p.B; b += kWave) {
+      const Request r = request(p, b);
+      if (wanted(p, r) > 0 && admitted(p, r, blocks[b + 1], tokens[b + 1])) taken = max(taken, blocks[b + 1]);
+    }
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) taken = max(taken, __shfl_xor(taken, o, kWave));
+    if (lane == 0) {
+      p.counts[0] = taken;
+      p.counts[1] = blocks[p.B];
+      p.counts[2] = tokens[p.B];
+    }
+  }
+  const int pairs = p.B * p.H;
+  for (int pair = group * kPairsPerGroup + wave; pair < min((group + 1) * kPairsPerGroup, pairs); pair += kWaves) {
+    const int b = pair / p.H, h = pair % p.H;
+    const Request r = request(p, b);
+    const bool ok = admitted(p, r, blocks[b + 1], tokens[b + 1]);
+    const int before = blocks_of(r.held, p.shift), n = ok ? wanted(p, r) : 0, first = blocks[b] + h * n;
+    int32_t* row = p.table + (int64_t)pair * p.per_seq;
+    const int from = p.held ? before : 0, to = p.held ? before + n : p.per_seq;      // a new table is written whole
+    for (int c = from + lane; c < to; c += kWave) {
+      int id = 0;
+      if (c - before < n) id = p.free_blocks ? p.free_blocks[first + c - before] : first + c - before;
+      row[c] = id;
+    }
+  }
+}
+
+}  // namespace
+
+int launch_block_tables(const vector_blocks& v, int32_t* table, int32_t* live, int64_t* slots, int64_t n_slots, int32_t* counts, hipStream_t stream) {
+  TableParams p = {};
+  p.held = v.len_held; p.len = v.len; p.free_blocks = v.free_blocks;
+  p.table = table; p.live = live; p.counts = counts; p.slots = n_slots > 0 ? slots : nullptr;
+  p.B = v.batch; p.H = v.n_kv_heads; p.per_seq = v.blocks_per_seq; p.n_free = v.n_free; p.n_slots = (int)n_slots;
+  while ((1 << p.shift) < v.block_rows) ++p.shift;
+  p.slot_groups = (p.n_slots + kTokensPerGroup - 1) / kTokensPerGroup;
+  const int table_groups = (p.B * p.H + kPairsPerGroup - 1) / kPairsPerGroup;
+  VEC_LAUNCH(K_BLOCK_TABLES, block_tables_kernel, dim3(p.slot_groups + table_groups), dim3(kThreads), 2 * (p.B + 1) * sizeof(int), stream, p);
+  VEC_HIP(hipGetLastError());
+  return VECTOR_OK;
+}
+
+}  // namespace vec

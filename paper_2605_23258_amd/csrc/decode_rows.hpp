@@ -164,6 +164,19 @@ inline bool pick_one_round(const SplitCosts& c, int batch, int n_kv_heads, int c
   return best >= 0.0;
 }
 
+// Caches held in 4 bits: as many workgroups as run at the same time, pieces of equal length in steps of 128 rows.
+constexpr int kFp4StepRows = 128, kFp4PerCu = 3;
+inline void pick_splits_fp4(int batch, int n_kv_heads, int cap_retain, int n_approx, int& s_ret, int& s_apx) {
+  const int64_t steps_r = ((int64_t)cap_retain + kFp4StepRows - 1) / kFp4StepRows, steps_a = ((int64_t)n_approx + kFp4StepRows - 1) / kFp4StepRows;
+  const int64_t pairs = (int64_t)batch * n_kv_heads, at_once = 256 * kFp4PerCu;
+  const int64_t most = std::max<int64_t>(2, std::min<int64_t>(kMaxSplits, at_once / pairs));
+  int64_t piece = std::max<int64_t>(1, (steps_r + steps_a + most - 1) / most);
+  while ((steps_r + piece - 1) / piece + (steps_a + piece - 1) / piece > most && piece < steps_r + steps_a) ++piece;
+  s_ret = (int)((steps_r + piece - 1) / piece);
+  s_apx = (int)((steps_a + piece - 1) / piece);
+  if (s_ret + s_apx == 0) s_ret = 1;             // nothing cached: one workgroup writes the empty partial
+}
+
 // Sequences of different lengths, whose live rows only the device knows, cut by a plan that the split launch makes (PlannedSplits in
 // decode_attn.hip): granules of 32 rows, four to a step; what the change to another segment costs, in granules (fitted to the workgroups'
 // ends: 0.5 us a granule with the chip full, 5 a change; 4, 6 and 9 measured); and how long a line of granules may be.

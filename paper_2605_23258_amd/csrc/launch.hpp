@@ -24,7 +24,7 @@ inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 // optional per-kernel event timing (timing.hip)
 enum KernelId { K_SCORE_STATS = 0, K_STATS_COMBINE, K_MASS_RESIDUAL, K_POOL, K_ROUTE, K_GATHER, K_DECODE_SPLIT,
-                K_DECODE_COMBINE, K_COUNT };
+                K_DECODE_COMBINE, K_FP4_ROWS, K_BLOCK_TABLES, K_COUNT };
 bool timing_enabled();
 void timing_begin(int id, hipStream_t stream);
 void timing_end(int id, hipStream_t stream);
@@ -188,5 +188,23 @@ size_t decode_workspace_bytes(int batch, int n_q_heads, int n_kv_heads, int head
 int launch_decode_attn(const vector_cache& c, const void* q, float scale, void* out, int flags, void* ws,
                        hipStream_t stream, const RopeParams* rope = nullptr, const void* k_new = nullptr,
                        const void* v_new = nullptr);
+
+// Caches held in 4 bits.  The rows of a layer for them: by lists (slots null), keys and values of the retained ones and keys of the
+// approximated ones; or n_retain rows in their own order by slots, into the pools k_ret and v_ret.
+struct Fp4Rows {
+  const void *k, *v;
+  const int32_t *idx_retain, *idx_approx;
+  const int64_t* slots;
+  int n_retain, n_approx, cap_retain;
+  int64_t pool_rows;
+  uint8_t *k_ret, *k_ret_scale, *v_ret, *v_ret_scale, *k_apx, *k_apx_scale;
+};
+int launch_store_fp4(const vector_shape& s, const Fp4Rows& rows, hipStream_t stream);
+int launch_load_fp4(int64_t n_rows, int head_dim, int dtype, const uint8_t* codes, const uint8_t* scales, int64_t pool_rows, const int64_t* slots,
+                    void* out, hipStream_t stream);
+int launch_decode_fp4(const vector_cache_fp4& c, const void* q, float scale, void* out, int flags, void* ws, hipStream_t stream,
+                      const RopeParams* rope, const void* k_new, const void* v_new);
+constexpr int kMaxRequests = 4096;
+int launch_block_tables(const vector_blocks& v, int32_t* table, int32_t* live, int64_t* slots, int64_t n_slots, int32_t* counts, hipStream_t stream);
 
 }  // namespace vec

@@ -17,7 +17,7 @@ struct Slot {
 bool g_enabled = false;
 Slot g_slots[K_COUNT];
 const char* const kNames[K_COUNT] = {"score_stats", "stats_combine", "mass_residual", "pool_scores",
-                                     "route", "gather_rows", "decode_split", "decode_combine"};
+                                     "route", "gather_rows", "decode_split", "decode_combine", "fp4_rows", "block_tables"};
 }  // namespace
 
 bool timing_enabled() { return g_enabled; }

@@ -597,6 +597,106 @@ int vector_decode_attn_rope(const vector_cache* c, const vector_rope* rope, cons
   return decode_checked(c, q, scale, out, flags, ws, ws_bytes, stream, &rp);
 }
 
+int vector_block_tables(const vector_blocks* b, int32_t* block_table, int32_t* len_live, int64_t* slots, int64_t n_slots, int32_t* counts,
+                        void* stream) {
+  if (!b || !b->len || !block_table || !len_live || !counts) return VECTOR_ERR_ARG;
+  if (b->batch < 1 || b->batch > vec::kMaxRequests || b->n_kv_heads < 1 || b->n_kv_heads > 65535) return VECTOR_ERR_SHAPE;
+  if (b->block_rows < 16 || (b->block_rows & (b->block_rows - 1)) || b->blocks_per_seq < 1 || b->n_free < 0) return VECTOR_ERR_ARG;
+  if ((int64_t)b->batch * b->n_kv_heads > INT32_MAX / b->blocks_per_seq) return VECTOR_ERR_SHAPE;
+  if (n_slots < 0 || n_slots >= INT32_MAX || (!slots && n_slots > 0)) return VECTOR_ERR_ARG;
+  if (len_live == b->len || len_live == b->len_held) return VECTOR_ERR_ARG;
+  return vec::launch_block_tables(*b, block_table, len_live, slots, n_slots, counts, (hipStream_t)stream);
+}
+
+static bool fp4_rows_ok(const uint8_t* codes, const uint8_t* scales) { return codes && scales && aligned16(codes) && aligned16(scales); }
+
+int vector_compact_fp4(const vector_shape* s, const void* k, const void* v, const int32_t* idx_retain, const int32_t* idx_approx,
+                       int32_t n_retain, int32_t n_approx, uint8_t* k_ret, uint8_t* k_ret_scale, uint8_t* v_ret, uint8_t* v_ret_scale,
+                       uint8_t* k_apx, uint8_t* k_apx_scale, int32_t cap_retain, void* stream) {
+  int rc = check_shape(s, false);
+  if (rc) return rc;
+  if (n_retain < 0 || n_approx < 0 || cap_retain < n_retain || (int64_t)n_retain + n_approx > s->seq_len) return VECTOR_ERR_ARG;
+  if (!k || !v || !aligned16(k) || !aligned16(v)) return VECTOR_ERR_ARG;
+  if (n_retain > 0 && (!idx_retain || !fp4_rows_ok(k_ret, k_ret_scale) || !fp4_rows_ok(v_ret, v_ret_scale))) return VECTOR_ERR_ARG;
+  if (n_approx > 0 && (!idx_approx || !fp4_rows_ok(k_apx, k_apx_scale))) return VECTOR_ERR_ARG;
+  const vec::Fp4Rows rows = {k, v, idx_retain, idx_approx, nullptr, n_retain, n_approx, cap_retain, 0,
+                             k_ret, k_ret_scale, v_ret, v_ret_scale, k_apx, k_apx_scale};
+  return vec::launch_store_fp4(*s, rows, (hipStream_t)stream);
+}
+
+int vector_store_fp4(const vector_shape* s, const void* k, const void* v, const int64_t* slots, int64_t pool_rows, uint8_t* k_pool,
+                     uint8_t* k_pool_scale, uint8_t* v_pool, uint8_t* v_pool_scale, void* stream) {
+  if (!s) return VECTOR_ERR_ARG;
+  vector_shape any_length = *s;                     // a batch of prompts may have more tokens than one sequence
+  if (s->seq_len > 1) any_length.seq_len = 1;
+  int rc = check_shape(&any_length, false);
+  if (rc) return rc;
+  if (!k || !slots || pool_rows < 0 || !aligned16(k) || !aligned16(v) || !fp4_rows_ok(k_pool, k_pool_scale)) return VECTOR_ERR_ARG;
+  if (v ? !fp4_rows_ok(v_pool, v_pool_scale) : (v_pool || v_pool_scale)) return VECTOR_ERR_ARG;
+  const vec::Fp4Rows rows = {k, v, nullptr, nullptr, slots, s->seq_len, 0, 0, pool_rows, k_pool, k_pool_scale, v_pool, v_pool_scale, nullptr, nullptr};
+  return vec::launch_store_fp4(*s, rows, (hipStream_t)stream);
+}
+
+int vector_load_fp4(int64_t n_rows, int32_t head_dim, int32_t dtype, const uint8_t* codes, const uint8_t* scales, int64_t pool_rows,
+                    const int64_t* slots, void* out, void* stream) {
+  if (dtype != VECTOR_F32 && dtype != VECTOR_BF16) return VECTOR_ERR_DTYPE;
+  if ((head_dim != 64 && head_dim != 128) || n_rows > ((int64_t)1 << 34)) return VECTOR_ERR_SHAPE;
+  if (n_rows < 0 || pool_rows < 0 || !out || !aligned16(out) || !fp4_rows_ok(codes, scales)) return VECTOR_ERR_ARG;
+  if (n_rows == 0) return VECTOR_OK;
+  return vec::launch_load_fp4(n_rows, head_dim, dtype, codes, scales, pool_rows, slots, out, (hipStream_t)stream);
+}
+
+// the shape of a cache in 4 bits: what the caches in 16 and 32 bits are held to
+static int check_fp4_cache(const vector_cache_fp4* c) {
+  if (!c) return VECTOR_ERR_ARG;
+  if (c->dtype != VECTOR_F32 && c->dtype != VECTOR_BF16) return VECTOR_ERR_DTYPE;
+  if (c->head_dim != 64 && c->head_dim != 128) return VECTOR_ERR_SHAPE;
+  if (c->batch < 1 || c->batch > 65535 || c->n_kv_heads < 1 || c->n_kv_heads > 65535) return VECTOR_ERR_SHAPE;
+  if (c->n_q_heads < c->n_kv_heads || c->n_q_heads % c->n_kv_heads) return VECTOR_ERR_SHAPE;
+  const int G = c->n_q_heads / c->n_kv_heads;
+  if (G > 8 && G != 10 && G != 12 && G != 16) return VECTOR_ERR_SHAPE;
+  return c->cap_retain < 0 || c->n_approx < 0 ? VECTOR_ERR_ARG : VECTOR_OK;
+}
+
+size_t vector_decode_fp4_workspace_bytes(const vector_cache_fp4* c) {
+  if (check_fp4_cache(c) != VECTOR_OK) return 0;
+  return vec::decode_workspace_bytes(c->batch, c->n_q_heads, c->n_kv_heads, c->head_dim, c->cap_retain, c->n_approx);
+}
+
+static int decode_fp4_checked(const vector_cache_fp4* c, const vector_rope* rope, const void* q, const void* k_new, const void* v_new, float scale,
+                              void* out, int32_t flags, void* ws, size_t ws_bytes, void* stream, bool step) {
+  int rc = check_fp4_cache(c);
+  if (rc) return rc;
+  vec::RopeParams rp;
+  if (rope && (rc = make_rope(rope, c->head_dim, rp))) return rc;
+  if (!q || !out || !aligned16(q) || !aligned16(out) || !c->len_retain) return VECTOR_ERR_ARG;
+  if (step && (!k_new || !v_new || !aligned16(k_new) || !aligned16(v_new) || c->cap_retain < 1)) return VECTOR_ERR_ARG;
+  if (flags & VECTOR_DECODE_LITERAL) return VECTOR_ERR_DTYPE;
+  if ((flags & ~VECTOR_DECODE_OUT_F32) || !(scale == scale)) return VECTOR_ERR_ARG;
+  const int n_seq_arrays = (c->cap_retain_seq != nullptr) + (c->n_approx_seq != nullptr) + (c->ret_row_start != nullptr) +
+                           (c->apx_row_start != nullptr);
+  if (n_seq_arrays != 0 && n_seq_arrays != 4) return VECTOR_ERR_ARG;
+  if (c->ret_block_table) {
+    const int rows = c->ret_block_rows;
+    if (n_seq_arrays != 0 || rows < 16 || (rows & (rows - 1)) || c->ret_blocks_per_seq < 1 || c->n_blocks < 0) return VECTOR_ERR_ARG;
+    if ((int64_t)c->cap_retain > (int64_t)c->ret_blocks_per_seq * rows) return VECTOR_ERR_ARG;
+  }
+  if (c->cap_retain > 0 && (!fp4_rows_ok(c->k_ret, c->k_ret_scale) || !fp4_rows_ok(c->v_ret, c->v_ret_scale))) return VECTOR_ERR_ARG;
+  if (c->n_approx > 0 && (!fp4_rows_ok(c->k_apx, c->k_apx_scale) || !c->W || !aligned16(c->W))) return VECTOR_ERR_ARG;
+  if ((rc = check_ws(ws, ws_bytes, vector_decode_fp4_workspace_bytes(c)))) return rc;
+  return vec::launch_decode_fp4(*c, q, scale, out, flags, ws, (hipStream_t)stream, rope ? &rp : nullptr, k_new, v_new);
+}
+
+int vector_decode_attn_fp4(const vector_cache_fp4* c, const vector_rope* rope, const void* q, float scale, void* out, int32_t flags, void* ws,
+                           size_t ws_bytes, void* stream) {
+  return decode_fp4_checked(c, rope, q, nullptr, nullptr, scale, out, flags, ws, ws_bytes, stream, false);
+}
+
+int vector_decode_step_fp4(const vector_cache_fp4* c, const vector_rope* rope, const void* q, const void* k_new, const void* v_new, float scale,
+                           void* out, int32_t flags, void* ws, size_t ws_bytes, void* stream) {
+  return decode_fp4_checked(c, rope, q, k_new, v_new, scale, out, flags, ws, ws_bytes, stream, true);
+}
+
 int vector_residual_rope(const vector_shape* s, const void* k, const void* v, const void* W, const vector_rope* rope,
                          float* eps, void* ws, size_t ws_bytes, void* stream) {
   (void)ws; (void)ws_bytes;
