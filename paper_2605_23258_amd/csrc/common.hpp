@@ -323,6 +323,10 @@ __device__ __forceinline__ void load_to_lds16(uint32_t lds, const void* g) {
 __device__ __forceinline__ void load_to_lds4(uint32_t lds, const void* g) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(__builtin_amdgcn_readfirstlane((int)lds)), "v"(g) : "m0", "memory");
 }
+// 64 lanes x 2 bytes, each into the low half of four
+__device__ __forceinline__ void load_to_lds2(uint32_t lds, const void* g) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_ushort %1, off" ::"s"(__builtin_amdgcn_readfirstlane((int)lds)), "v"(g) : "m0", "memory");
+}
 template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 
 }  // namespace vec

@@ -7,16 +7,16 @@
 // an element in 4 bits times its scale has two significant bits and is a bf16 number exactly, so the only
 // roundings are those of the weights, which go in as parts of eight bits each (kParts).
 //
-// Nothing passes through LDS before the end and no wave waits for another: a wave takes 32 rows at a time, and both operands come
-// straight from memory in the matrix cores' order.
-//   scores   S[t][g] = sum_e K[t][e] q[g][e]      A = K: lane (m, quarter) holds D / 4 consecutive elements of a row, which is one load and
+// A wave takes 32 rows at a time and waits for no other before the end.  Their codes and scales go from memory straight into a ring of its
+// own in LDS (Fp4Stage), so that what is on its way takes no registers, and are read back in the matrix cores' order:
+//   scores   S[t][g] = sum_e K[t][e] q[g][e]      A = K: lane (m, quarter) holds D / 4 consecutive elements of a row, which is one read and
 //                                                  one scale; B = the query rows in the same order of e
 //   output   O[j][g] += sum_t R[t][j] P[t][g]     A = R^T: lane (m, quarter) holds dims D / 16 m .. of eight rows, 8 quarter ..; the conversion
 //                                                  hands out two neighbouring dims of one row, and a byte permutation makes
 //                                                  two rows of one dim of them
 // Row 4 a + i of score tile u is token 8 a + 4 u + i, so that the eight weights that a lane gets from both score tiles are those
-// of the eight rows that it holds of R.  R is the values, or for approximated rows the keys, loaded a second time in the other order
-// (from the caches); under ROPE these are turned back by their positions first.
+// of the eight rows that it holds of R.  R is the values, or for approximated rows the keys, read a second time in the other order;
+// under ROPE these are turned back by their positions first.
 //
 // Sixteen columns hold up to 16 query rows.  Up to eight (SIDE): columns g take the weights' leading bits and columns 8 + g what these leave,
 // with one product for both.
@@ -37,6 +37,20 @@ struct Fp4Params {
 constexpr int kFp4TileRows = 32;
 constexpr float kRaiseAt = 16.f;       // log2: how far a score may lie above its column's reference before that is raised
 
+// no more than n loads on their way; n is the same for the wave
+__device__ __forceinline__ void wait_tiles(int n) {
+  switch (n) {
+    case 0: wait_loads<0>(); break;
+    case 2: wait_loads<2>(); break;
+    case 3: wait_loads<3>(); break;
+    case 4: wait_loads<4>(); break;
+    case 5: wait_loads<5>(); break;
+    case 6: wait_loads<6>(); break;
+    case 10: wait_loads<10>(); break;
+    default: wait_loads<0>();
+  }
+}
+
 // rounds a weight to its leading eight bits by cutting the others off: what is left is exact
 __device__ __forceinline__ float leading(float x) { return __uint_as_float(__float_as_uint(x) & 0xffff0000u); }
 // two floats with no more than eight significant bits as two bf16
@@ -44,13 +58,22 @@ __device__ __forceinline__ uint32_t high_halves(float lo, float hi) {
   return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
 }
 
-template <int D> struct Fp4Tile {
-  static constexpr int kWords = D / 32;      // of a lane's part of a key row
-  uint32_t k[2][kWords], k_unit[2];          // scales as they are, a byte
-  uint32_t r[8];                             // codes of D / 16 dims of eight rows
-  u32x4 r_unit[D / 64];                      // scale bytes of these rows, D / 32 a row
-  uint32_t dead;                             // bit j: row j of the eight is none
+// Where a tile of 32 rows lies in LDS.  Row 8 a + b of it is the (4 b + a)-th, so that the four rows that a wave reads at once of R, one for each
+// quarter, are neighbours, and the 16-byte pieces of a row are permuted by b, so that the keys' 16-byte reads of rows b, b + 1, .. hit
+// distinct banks.  A scale slot holds the scale bytes of a row (keys' rows, then R's;
+// of approximated rows, which have one tensor, the positions in the place of the latter).
+template <int D> struct Fp4Stage {
+  static constexpr int kCode = fp4_code_bytes(D), kPieces = kCode / 16;
+  static constexpr int kTensor = kFp4TileRows * kCode;
+  static constexpr int kSlots = 2 * kTensor, kPositions = kSlots + 128, kAlive = kSlots + 256;
+  static constexpr int kBytes = kAlive + 16;
+  static constexpr int kLoads = kTensor / 1024;                 // wave-wide loads of a tensor
+  static constexpr int kRowsPerLoad = kFp4TileRows / kLoads;
+  static __device__ __forceinline__ int place(int row) { return 4 * (row & 7) + (row >> 3); }
+  static __device__ __forceinline__ int twist(int place) { return D == 128 ? (place >> 2) & 3 : (place >> 3) & 1; }
+  static __device__ __forceinline__ int piece(int row, int piece) { return place(row) * kCode + ((piece ^ twist(place(row))) * 16); }
 };
+constexpr int kFp4Stages = 3;
 
 // T: of the query, W, the output and the step's token.  SIDE: no more than eight query rows, T bf16.
 template <typename T, int D, bool SIDE, bool ROPE>
@@ -63,6 +86,7 @@ __device__ __forceinline__ void attend_fp4(const Fp4Params& f, const RopeParams&
   constexpr int kRedStride = D + 4;
   constexpr float kNegBig = -1.0e30f;                  // reference before any row: finite, so differences stay finite
   constexpr int kStepRows = DW * kFp4TileRows;
+  typedef Fp4Stage<D> St;
 
   const DecodeParams& p = f.d;
   const int G = p.Hq / p.Hkv, PSZ = 2 * G + G * D;
@@ -74,7 +98,6 @@ __device__ __forceinline__ void attend_fp4(const Fp4Params& f, const RopeParams&
   const size_t bh = (size_t)range.b * p.Hkv + range.h;
   // rows in memory: the step's own token, the last live row, comes from the caller's tensors
   const int stored = is_apx ? seg.n_approx : seg.new_row >= 0 ? seg.new_row : seg.len_retain;
-  const int live = is_apx ? seg.n_approx : seg.len_retain;
   const int new_row = is_apx ? -1 : seg.new_row;
   const uint8_t* k_codes = reinterpret_cast<const uint8_t*>(is_apx ? p.k_apx : p.k_ret);
   const uint8_t* k_scales = is_apx ? f.k_apx_scale : f.k_ret_scale;
@@ -86,6 +109,11 @@ __device__ __forceinline__ void attend_fp4(const Fp4Params& f, const RopeParams&
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
   };
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+  auto wave_fence = []() VEC_INLINE {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  };
 
   // query rows: column m holds row m, or m % 8
   u32x4 qf[kQueryParts][NC];
@@ -118,150 +146,119 @@ __device__ __forceinline__ void attend_fp4(const Fp4Params& f, const RopeParams&
 
   // paged: ids of the blocks from window on, one a lane
   int window = row_begin >> seg.block_shift, ids = 0;
-  auto load_window = [&]() VEC_INLINE { ids = seg.blocks[min(window + lane, p.blocks_per_seq - 1)]; };
-  if (paged) load_window();
-  // first row, in the pools, of the tile's 16 rows from `row` on; false: there are none
+  auto load_window = [&]() VEC_INLINE {
+    ids = seg.blocks[min(window + lane, p.blocks_per_seq - 1)];
+    asm volatile("" : "+v"(ids));                    // waited for here, and not wherever it is used
+  };
+  if (paged && row_begin < row_end) load_window();
+  // first row, in the pools, of the rows from `row` on; false: there are none
   auto block_row = [&](int row, int64_t& at) VEC_INLINE {
     const int id = __builtin_amdgcn_readlane(ids, (row >> seg.block_shift) - window);
     at = ((int64_t)id << seg.block_shift) + (row & ((1 << seg.block_shift) - 1));
     return (uint32_t)id < (uint32_t)f.n_blocks && (row >> seg.block_shift) < p.blocks_per_seq;
   };
 
-  // rows of a lane inside a tile: of the key tiles (+ 4 for the second one), the first of the eight of R
-  const int k_row = 8 * (m >> 2) + (m & 3), r_row = 8 * quarter;
-  auto load_key = [&](Fp4Tile<D>& t, int u, int64_t row) VEC_INLINE {
-    if constexpr (D == 128) {
-      const u32x4 x = *reinterpret_cast<const u32x4*>(k_codes + row * kCode + quarter * 16);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) t.k[u][i] = x[i];
-      t.k_unit[u] = k_scales[row * kScale + quarter];
-    } else {
-      const u32x2 x = *reinterpret_cast<const u32x2*>(k_codes + row * kCode + quarter * 8);
-      t.k[u][0] = x[0];
-      t.k[u][1] = x[1];
-      t.k_unit[u] = k_scales[row * kScale + (quarter >> 1)];
-    }
-  };
-  auto load_r = [&](int64_t row) VEC_INLINE {
-    if constexpr (D == 128) return *reinterpret_cast<const uint32_t*>(r_codes + row * kCode + m * 4);
-    else return (uint32_t)*reinterpret_cast<const uint16_t*>(r_codes + row * kCode + m * 2);
-  };
-  // codes and scale of a block of the step's token, elements first .. first + 7 of it
-  auto new_codes = [&](const void* token, int block, int first, uint32_t& byte) VEC_INLINE {
-    const T* x = reinterpret_cast<const T*>(token) + bh * D + block * kFp4Block;
-    uint32_t top = 0;
-    float y[8];
-#pragma unroll
-    for (int i = 0; i < kFp4Block; i += 8) { load8(x + i, y); top = max(top, top_bits8(y)); }
-    byte = fp4_scale_byte(top);
-    load8(x + first, y);
-    return fp4_codes(y, byte);
-  };
+  extern __shared__ __align__(16) unsigned char fp4_lds[];
+  unsigned char* ring = fp4_lds + wave * (kFp4Stages * St::kBytes);
+  const int32_t* positions = (ROPE && is_apx && rp.positions) ? rp.positions + seg.apx_row0 : nullptr;
+  const bool turned = ROPE && is_apx;
+  // what a lane brings in: a 16-byte piece of codes of one row (a load), and of one more kRowsPerLoad / 4 further on in every eight (the next
+  // load); the scales of one row
+  const int in_place = lane / St::kPieces, in_row = 8 * (in_place & 3) + (in_place >> 2);
+  const int in_piece = (lane % St::kPieces) ^ St::twist(in_place);
+  // (the second load's places are 16 further on, which the permutation does not see)
+  const int scale_row = lane & 31;
+  bool holes = false;                                  // a block that does not exist has been met
 
-  auto fetch = [&](Fp4Tile<D>& t, int base) VEC_INLINE {
-    int64_t k_at = row0 + base, r_at = row0 + base;         // of the tile's first row, or (blocks of 16 rows) of the lane's half
-    bool there = true, k_there = true, r_there = true;
+  auto fill = [&](int base, unsigned char* st) VEC_INLINE {
+    int64_t at_lo = row0 + base, at_hi = at_lo;        // of the tile's first row, less 16 rows of its 17th
+    bool lo = true, hi = true;
     if (paged) {
       if (((base + kFp4TileRows - 1) >> seg.block_shift) - window > kWave - 1) { window = base >> seg.block_shift; load_window(); }
-      int64_t at[2];
-      bool ok[2];
-      ok[0] = block_row(base, at[0]);
-      if (seg.block_shift >= 5) {
-        k_at = r_at = at[0];
-        there = k_there = r_there = ok[0];
-      } else {
-        ok[1] = block_row(base + 16, at[1]);
-        at[1] -= 16;
-        there = ok[0] && ok[1];
-        k_at = (m >> 3) ? at[1] : at[0];
-        r_at = (quarter >> 1) ? at[1] : at[0];
-        k_there = (m >> 3) ? ok[1] : ok[0];
-        r_there = (quarter >> 1) ? ok[1] : ok[0];
+      lo = hi = block_row(base, at_lo);
+      at_hi = at_lo;
+      if (seg.block_shift < 5) {
+        hi = block_row(base + 16, at_hi);
+        at_hi -= 16;
       }
     }
-    t.dead = 0;
-    if (base + kFp4TileRows <= stored && there) {           // uniform: rows that are all there
+    const uint32_t to = lds_address(st);
+    if (base + kFp4TileRows <= stored && lo && hi) {   // uniform: rows that are all there
+      const int64_t row = (in_row < 16 ? at_lo : at_hi) + in_row;
+      const uint8_t* k = k_codes + row * kCode + in_piece * 16;
 #pragma unroll
-      for (int u = 0; u < 2; ++u) load_key(t, u, k_at + k_row + 4 * u);
+      for (int i = 0; i < St::kLoads; ++i) load_to_lds16(to + i * 1024, k + i * (8 / St::kLoads) * kCode);
+      if (!is_apx) {
+        const uint8_t* r = r_codes + row * kCode + in_piece * 16;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) t.r[j] = load_r(r_at + r_row + j);
-      const uint8_t* s = r_scales + (r_at + r_row) * kScale;
-      if constexpr (D == 128) {
-        t.r_unit[0] = *reinterpret_cast<const u32x4_a4*>(s);
-        t.r_unit[1] = *reinterpret_cast<const u32x4_a4*>(s + 16);
-      } else {
-        t.r_unit[0] = *reinterpret_cast<const u32x4_a2*>(s);
+        for (int i = 0; i < St::kLoads; ++i) load_to_lds16(to + St::kTensor + i * 1024, r + i * (8 / St::kLoads) * kCode);
       }
+      const void* s = (lane < 32 ? k_scales : r_scales) + ((scale_row < 16 ? at_lo : at_hi) + scale_row) * kScale;
+      if (!turned) {
+        if constexpr (D == 128) load_to_lds4(to + St::kSlots, s);
+        else load_to_lds2(to + St::kSlots, s);
+      } else {
+        if (positions && D == 128 && lane >= 32) s = positions + base + scale_row;
+        if (lane < 32 || (positions && D == 128)) {
+          if constexpr (D == 128) load_to_lds4(to + St::kSlots, s);
+          else load_to_lds2(to + St::kSlots, s);
+        }
+        if (lane < 32) {
+          if (!positions) *reinterpret_cast<int*>(st + St::kPositions + lane * 4) = base + lane;
+          else if (D != 128) load_to_lds4(to + St::kPositions, positions + base + lane);
+        }
+      }
+      if (holes && lane == 0) *reinterpret_cast<uint32_t*>(st + St::kAlive) = ~0u;
       return;
     }
-    // The last rows, rows of blocks that do not exist, the step's own token: row by row.  What is no row is all zeros, since a
-    // weight of 0 does not make a NaN of the memory harmless.
+    // The last rows, rows of blocks that do not exist, the step's own token.  What is no row is all zeros, since a weight of 0 does
+    // not make a NaN of the memory harmless.
+    wait_loads<0>();                                   // the count of what is on its way starts anew behind this tile
+    holes = holes || !lo || !hi;
+    {
+      const int row = lane & 31, half = lane >> 5;     // two lanes a row
+      const bool is = base + row < stored && (row < 16 ? lo : hi);
+      const int64_t at = (row < 16 ? at_lo : at_hi) + row;
+      for (int t = 0; t < (is_apx ? 1 : 2); ++t) {
+        const uint8_t* codes = t ? r_codes : k_codes;
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int row = base + k_row + 4 * u;
-      t.k_unit[u] = 0;
-#pragma unroll
-      for (int i = 0; i < Fp4Tile<D>::kWords; ++i) t.k[u][i] = 0;
-      if (row < stored && k_there) load_key(t, u, k_at + k_row + 4 * u);
-      if (row == new_row) {
-        constexpr int kBlockOf = D == 128 ? 1 : 2;           // lanes of a block
-        const int block = quarter / kBlockOf, inside = quarter % kBlockOf * 16;
-        uint32_t byte = 0;
-#pragma unroll
-        for (int i = 0; i < Fp4Tile<D>::kWords; ++i) t.k[u][i] = new_codes(p.k_new, block, inside + 8 * i, byte);
-        t.k_unit[u] = byte;
-        if (new_row < seg.cap && k_there) {
-          const int64_t at = k_at + k_row + 4 * u;
-          uint8_t* codes = const_cast<uint8_t*>(k_codes) + at * kCode + quarter * (D / 8);
-#pragma unroll
-          for (int i = 0; i < Fp4Tile<D>::kWords; ++i) reinterpret_cast<uint32_t*>(codes)[i] = t.k[u][i];
-          if (quarter % kBlockOf == 0) const_cast<uint8_t*>(k_scales)[at * kScale + block] = (uint8_t)byte;
+        for (int i = 0; i < St::kPieces / 2; ++i) {
+          const int piece = half * (St::kPieces / 2) + i;
+          u32x4 x = {0u, 0u, 0u, 0u};
+          if (is) x = *reinterpret_cast<const u32x4*>(codes + at * kCode + piece * 16);
+          *reinterpret_cast<u32x4*>(st + t * St::kTensor + St::piece(row, piece)) = x;
         }
       }
+      // the scales of both tensors, one a lane
+      const uint8_t* s = (half ? r_scales : k_scales) + at * kScale;
+      uint32_t unit = 0;
+      if (is) unit = D == 128 ? *reinterpret_cast<const uint32_t*>(s) : (uint32_t)*reinterpret_cast<const uint16_t*>(s);
+      if (turned && half == 1) unit = is ? (uint32_t)(positions ? positions[base + row] : base + row) : 0u;
+      *reinterpret_cast<uint32_t*>(st + St::kSlots + lane * 4) = unit;
+      const uint32_t alive = (uint32_t)__ballot(is || base + row == new_row);           // bit r: row r is one
+      if (lane == 0) *reinterpret_cast<uint32_t*>(st + St::kAlive) = alive;
     }
-    uint32_t unit[D == 128 ? 8 : 4];
-#pragma unroll
-    for (int j = 0; j < (D == 128 ? 8 : 4); ++j) unit[j] = 0;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int row = base + r_row + j;
-      uint32_t scales = 0;                                    // the row's, of all blocks
-      t.r[j] = 0;
-      if (row < stored && r_there) {
-        t.r[j] = load_r(r_at + r_row + j);
-        const uint8_t* s = r_scales + (r_at + r_row + j) * kScale;
-        if constexpr (D == 128) scales = *reinterpret_cast<const uint32_t*>(s);
-        else scales = *reinterpret_cast<const uint16_t*>(s);
-      } else if (row != new_row) {
-        t.dead |= 1u << j;
+    wave_fence();
+    if (new_row >= base && new_row < base + kFp4TileRows && lane < D / 4) {
+      // eight elements of the token's key or value a lane, as vector_store_fp4 rounds them
+      constexpr int kLanes = D / 8;
+      const int t = lane / kLanes, i = lane % kLanes, row = new_row - base;
+      float x[8];
+      load8(reinterpret_cast<const T*>(t ? p.v_new : p.k_new) + bh * D + i * 8, x);
+      const uint32_t byte = fp4_scale_byte(quad_max(top_bits8(x))), codes = fp4_codes(x, byte);
+      *reinterpret_cast<uint32_t*>(st + t * St::kTensor + St::piece(row, i / 4) + i % 4 * 4) = codes;
+      if (i % 4 == 0) st[St::kSlots + (t * 32 + row) * 4 + i / 4] = (uint8_t)byte;
+      if (new_row < seg.cap && (row < 16 ? lo : hi)) {
+        const int64_t at = (row < 16 ? at_lo : at_hi) + row;
+        *reinterpret_cast<uint32_t*>(const_cast<uint8_t*>(t ? r_codes : k_codes) + at * kCode + i * 4) = codes;
+        if (i % 4 == 0) const_cast<uint8_t*>(t ? r_scales : k_scales)[at * kScale + i / 4] = (uint8_t)byte;
       }
-      if (row == new_row) {
-        const int block = m / (16 / kScale), inside = m % (16 / kScale) * (D / 16);
-        uint32_t byte = 0, codes = new_codes(p.v_new, block, inside & ~7, byte);
-        if constexpr (D == 64) codes = codes >> (m & 1) * 16 & 0xffffu;
-        t.r[j] = codes;
-        scales = byte << 8 * block;
-        if (new_row < seg.cap && r_there) {
-          const int64_t at = r_at + r_row + j;
-          uint8_t* to = const_cast<uint8_t*>(r_codes) + at * kCode + m * (D / 32);
-          if constexpr (D == 128) *reinterpret_cast<uint32_t*>(to) = codes;
-          else *reinterpret_cast<uint16_t*>(to) = (uint16_t)codes;
-          if (inside == 0) const_cast<uint8_t*>(r_scales)[at * kScale + block] = (uint8_t)byte;
-        }
-      }
-      if constexpr (D == 128) unit[j] = scales;
-      else unit[j / 2] |= scales << (j & 1) * 16;
     }
-#pragma unroll
-    for (int j = 0; j < (D == 128 ? 8 : 4); ++j) t.r_unit[j / 4][j % 4] = unit[j];
   };
 
-  // the scale of row j of the eight, for the lane's dims
+  // a lane's rows of a tile in operand order: the key row (and that four further on), the first of the eight of R
+  const int k_row = 8 * (m >> 2) + (m & 3), r_row = 8 * quarter;
   const int my_block = m / (16 / kScale);
-  auto row_unit = [&](const Fp4Tile<D>& t, int j) VEC_INLINE {
-    const uint32_t word = D == 128 ? t.r_unit[j / 4][j % 4] : t.r_unit[0][j / 2] >> (j & 1) * 16;
-    return fp4_unit(word >> 8 * my_block & 0xffu);
-  };
 
   // under ROPE a lane's dims always belong to the same rotary pairs
   constexpr int kDims = D / 16;
@@ -276,18 +273,27 @@ __device__ __forceinline__ void attend_fp4(const Fp4Params& f, const RopeParams&
       }
     }
   }
-  const int32_t* positions = (ROPE && is_apx && rp.positions) ? rp.positions + seg.apx_row0 : nullptr;
-
-  auto consume = [&](const Fp4Tile<D>& t, int base) VEC_INLINE {
+  auto consume = [&](const unsigned char* st, int base) VEC_INLINE {
     // scores, in the log2 domain
     float s[8];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      const float unit = fp4_unit(t.k_unit[u]);
+      const int row = k_row + 4 * u;
+      uint32_t words[NC];
+      if constexpr (D == 128) {
+        const u32x4 x = *reinterpret_cast<const u32x4*>(st + St::piece(row, quarter));
+#pragma unroll
+        for (int c = 0; c < NC; ++c) words[c] = x[c];
+      } else {
+        const u32x2 x = *reinterpret_cast<const u32x2*>(st + St::piece(row, quarter >> 1) + (quarter & 1) * 8);
+#pragma unroll
+        for (int c = 0; c < NC; ++c) words[c] = x[c];
+      }
+      const float unit = fp4_unit(st[St::kSlots + row * 4 + (D == 128 ? quarter : quarter >> 1)]);
       f32x4 acc = zero;
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
-        const uint32_t w = t.k[u][c];
+        const uint32_t w = words[c];
         const u32x4 a = {fp4_pair_bf16<0>(w, unit), fp4_pair_bf16<1>(w, unit), fp4_pair_bf16<2>(w, unit), fp4_pair_bf16<3>(w, unit)};
 #pragma unroll
         for (int part = 0; part < kQueryParts; ++part) acc = mfma(a, qf[part][c], acc);
@@ -295,9 +301,10 @@ __device__ __forceinline__ void attend_fp4(const Fp4Params& f, const RopeParams&
 #pragma unroll
       for (int i = 0; i < 4; ++i) s[4 * u + i] = acc[i] * p.c2;
     }
-    if (__ballot(t.dead != 0)) {
+    if (holes || base + kFp4TileRows > stored) {
+      const uint32_t alive = *reinterpret_cast<const uint32_t*>(st + St::kAlive) >> r_row;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) s[j] = (t.dead >> j & 1) ? -INFINITY : s[j];
+      for (int j = 0; j < 8; ++j) s[j] = (alive >> j & 1) ? s[j] : -INFINITY;
     }
     float top = s[0];
 #pragma unroll
@@ -335,14 +342,28 @@ __device__ __forceinline__ void attend_fp4(const Fp4Params& f, const RopeParams&
 #pragma unroll
       for (int i = 0; i < 4; ++i) weights[part][i] = SIDE ? pack_bf16(y[2 * i], y[2 * i + 1]) : high_halves(y[2 * i], y[2 * i + 1]);
     }
+    // the eight rows of R, and their scales for the lane's dims
+    uint32_t r[8];
     float unit[8];
+    const unsigned char* rt = st + (is_apx ? 0 : St::kTensor);
+    const unsigned char* slots = st + St::kSlots + (is_apx ? 0 : 128);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) unit[j] = row_unit(t, j);
+    for (int j = 0; j < 8; ++j) {
+      const int at = St::piece(r_row + j, D == 128 ? m >> 2 : m >> 3);
+      if constexpr (D == 128) r[j] = *reinterpret_cast<const uint32_t*>(rt + at + (m & 3) * 4);
+      else r[j] = *reinterpret_cast<const uint16_t*>(rt + at + (m & 7) * 2);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; j += 4) {
+      const u32x4 x = *reinterpret_cast<const u32x4*>(slots + (r_row + j) * 4);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) unit[j + i] = fp4_unit(x[i] >> 8 * my_block & 0xffu);
+    }
     if (!ROPE || !is_apx) {
       for_each_constant<kDims / 2>([&](auto c) VEC_INLINE {
         uint32_t two[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) two[j] = fp4_pair_bf16<decltype(c)::value>(t.r[j], unit[j]);
+        for (int j = 0; j < 8; ++j) two[j] = fp4_pair_bf16<decltype(c)::value>(r[j], unit[j]);
         u32x4 even, odd;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -362,15 +383,12 @@ __device__ __forceinline__ void attend_fp4(const Fp4Params& f, const RopeParams&
       constexpr int kRowParts = kExact ? 3 : 1;
       float pos[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int row = min(base + r_row + j, live - 1);
-        pos[j] = (float)((positions ? positions[row] : row) + rp.pos_offset);
-      }
+      for (int j = 0; j < 8; ++j) pos[j] = (float)(*reinterpret_cast<const int*>(st + St::kPositions + (r_row + j) * 4) + rp.pos_offset);
       for_each_constant<kDims / 2>([&](auto c) VEC_INLINE {
         f32x2 two[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          f32x2 x = fp4_pair_f32<decltype(c)::value>(t.r[j], unit[j]);
+          f32x2 x = fp4_pair_f32<decltype(c)::value>(r[j], unit[j]);
           if (rp.interleaved) {
             float cs, sn;
             rotary_cos_sin(pos[j], t_hi[2 * c], t_lo[2 * c], cs, sn);
@@ -412,20 +430,37 @@ __device__ __forceinline__ void attend_fp4(const Fp4Params& f, const RopeParams&
     }
   };
 
-  int base = row_begin + wave * kFp4TileRows;
-  Fp4Tile<D> next;
-  if (base < row_end) fetch(next, base);
-  while (base < row_end) {
-    const Fp4Tile<D> tile = next;
-    const int then = base + kStepRows;
-    if (then < row_end) fetch(next, then);           // in flight while this tile is consumed
-    consume(tile, base);
-    base = then;
+  // loads of a tile; of tiles that went by the other way there are none on their way, nor of any before these
+  const int per_tile = is_apx ? St::kLoads + 1 + (D == 64 && turned && positions ? 1 : 0) : 2 * St::kLoads + 1;
+  static_assert(kFp4Stages == 3, "two tiles on their way while one is worked on");
+  const int tiles = row_begin + wave * kFp4TileRows < row_end ? (row_end - row_begin - wave * kFp4TileRows + kStepRows - 1) / kStepRows : 0;
+  const int first = row_begin + wave * kFp4TileRows;
+  if (tiles > 0) fill(first, ring);
+  if (tiles > 1) fill(first + kStepRows, ring + St::kBytes);
+  // The query rows have arrived from here on.  Without this the wait for them would sit in the loop, and wait for tiles as well.
+#pragma unroll
+  for (int part = 0; part < kQueryParts; ++part)
+#pragma unroll
+    for (int c = 0; c < NC; ++c) asm volatile("" : "+v"(qf[part][c]));
+  int stage = 0;
+  for (int i = 0; i < tiles; ++i) {
+    const int base = first + i * kStepRows;
+    // the stage of the tile before is free: what was read of it is in registers
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if (i + 2 < tiles) fill(base + 2 * kStepRows, ring + (stage == 0 ? 2 : stage - 1) * St::kBytes);
+    wait_tiles(per_tile * min(2, tiles - 1 - i));
+    wave_fence();
+    consume(ring + stage * St::kBytes, base);
+    stage = stage == 2 ? 0 : stage + 1;
   }
 
   // ---- merge the waves ----
-  __shared__ float red[DW][16][kRedStride];
-  __shared__ float ml[DW][2][16];
+  // a wave's sums in the place of its own ring
+  constexpr int kWaveBytes = kFp4Stages * St::kBytes;
+  static_assert(16 * kRedStride * 4 + 2 * 16 * 4 <= kWaveBytes, "the merge area must fit in the ring");
+  auto red = [&](int wv, int col, int j) VEC_INLINE { return reinterpret_cast<float*>(fp4_lds + wv * kWaveBytes) + col * kRedStride + j; };
+  auto ml = [&](int wv, int what, int col) VEC_INLINE { return reinterpret_cast<float*>(fp4_lds + wv * kWaveBytes) + 16 * kRedStride + what * 16 + col; };
+  wave_fence();
   float l_tot = l_run + __shfl_xor(l_run, 16, kWave);
   l_tot += __shfl_xor(l_tot, 32, kWave);
   // lane (m, quarter): column m, dims kDims * (4 quarter + i) + j
@@ -433,10 +468,10 @@ __device__ __forceinline__ void attend_fp4(const Fp4Params& f, const RopeParams&
   for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int j = 0; j < NT; j += 4)
-      *reinterpret_cast<f32x4*>(&red[wave][m][kDims * (4 * quarter + i) + j]) = f32x4{o[j][i], o[j + 1][i], o[j + 2][i], o[j + 3][i]};
+      *reinterpret_cast<f32x4*>(red(wave, m, kDims * (4 * quarter + i) + j)) = f32x4{o[j][i], o[j + 1][i], o[j + 2][i], o[j + 3][i]};
   if (quarter == 0) {
-    ml[wave][0][m] = l_tot > 0.f ? ref : -INFINITY;    // a wave without rows: its share is 0 without a branch
-    ml[wave][1][m] = l_tot;
+    *ml(wave, 0, m) = l_tot > 0.f ? ref : -INFINITY;    // a wave without rows: its share is 0 without a branch
+    *ml(wave, 1, m) = l_tot;
   }
   __syncthreads();
   float* out = p.part + range.slot * PSZ;
@@ -444,17 +479,17 @@ __device__ __forceinline__ void attend_fp4(const Fp4Params& f, const RopeParams&
     const int g = i / D, j = i % D;
     float top = -INFINITY, l = 0.f;
 #pragma unroll
-    for (int wv = 0; wv < DW; ++wv) top = fmaxf(top, ml[wv][0][g]);
+    for (int wv = 0; wv < DW; ++wv) top = fmaxf(top, *ml(wv, 0, g));
     const float safe = top == -INFINITY ? 0.f : top;
     f32x4 a = zero;
 #pragma unroll
     for (int wv = 0; wv < DW; ++wv) {
-      const float sc = fast_exp2(ml[wv][0][g] - safe);
-      f32x4 x = *reinterpret_cast<const f32x4*>(&red[wv][g][j]);
-      if constexpr (SIDE) x += *reinterpret_cast<const f32x4*>(&red[wv][8 + g][j]);
+      const float sc = fast_exp2(*ml(wv, 0, g) - safe);
+      f32x4 x = *reinterpret_cast<const f32x4*>(red(wv, g, j));
+      if constexpr (SIDE) x += *reinterpret_cast<const f32x4*>(red(wv, 8 + g, j));
 #pragma unroll
       for (int e = 0; e < 4; ++e) a[e] = fmaf(x[e], sc, a[e]);
-      l = fmaf(ml[wv][1][g], sc, l);
+      l = fmaf(*ml(wv, 1, g), sc, l);
     }
     *reinterpret_cast<f32x4_u*>(out + 2 * G + i) = a;
     if (j == 0) {
@@ -465,14 +500,16 @@ __device__ __forceinline__ void attend_fp4(const Fp4Params& f, const RopeParams&
 }
 
 template <typename T, int D, bool SIDE, bool ROPE>
-__global__ __launch_bounds__(DT_, 2) void decode_split_fp4_kernel(Fp4Params f, RopeParams rp) {
+__global__ __launch_bounds__(DT_, 3) void decode_split_fp4_kernel(Fp4Params f, RopeParams rp) {
   attend_fp4<T, D, SIDE, ROPE>(f, rp, grid_split<DW * kFp4TileRows>(f.d), (int)threadIdx.x);
 }
 
 template <typename T, int D, bool SIDE, bool ROPE>
 int launch_split_fp4(const Fp4Params& f, const RopeParams* rope, hipStream_t stream) {
   const dim3 grid(f.d.splits_ret + f.d.splits_apx, f.d.Hkv, f.d.B);
-  VEC_LAUNCH(K_DECODE_SPLIT, (decode_split_fp4_kernel<T, D, SIDE, ROPE>), grid, dim3(DT_), 0, stream, f, rope ? *rope : RopeParams{});
+  constexpr int lds = DW * kFp4Stages * Fp4Stage<D>::kBytes;
+  VEC_HIP(set_max_lds(reinterpret_cast<const void*>(decode_split_fp4_kernel<T, D, SIDE, ROPE>), lds));
+  VEC_LAUNCH(K_DECODE_SPLIT, (decode_split_fp4_kernel<T, D, SIDE, ROPE>), grid, dim3(DT_), lds, stream, f, rope ? *rope : RopeParams{});
   VEC_HIP(hipGetLastError());
   return VECTOR_OK;
 }

@@ -70,4 +70,10 @@ __device__ __forceinline__ uint32_t top_bits8(const float* x) {
   return top;
 }
 
+// the largest of four adjacent lanes
+__device__ __forceinline__ uint32_t quad_max(uint32_t x) {
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0xb1, 0xf, 0xf, false));    // lanes 1 0 3 2 of the four
+  return max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x4e, 0xf, 0xf, false));  // lanes 2 3 0 1
+}
+
 }  // namespace vec
