@@ -32,6 +32,7 @@ struct Fp4Params {
   DecodeParams d;
   const uint8_t *k_ret_scale, *v_ret_scale, *k_apx_scale;
   int n_blocks;                  // paged: of the pools
+  uint32_t flip;                 // 0x80000000: the scale is negative, and query rows change their sign (d.c2 is its size, above 0)
 };
 
 constexpr int kFp4TileRows = 32;
@@ -46,7 +47,9 @@ __device__ __forceinline__ void wait_tiles(int n) {
     case 4: wait_loads<4>(); break;
     case 5: wait_loads<5>(); break;
     case 6: wait_loads<6>(); break;
+    case 9: wait_loads<9>(); break;
     case 10: wait_loads<10>(); break;
+    case 18: wait_loads<18>(); break;
     default: wait_loads<0>();
   }
 }
@@ -75,8 +78,12 @@ template <int D> struct Fp4Stage {
 };
 constexpr int kFp4Stages = 3;
 
+// Rows of a workgroup: of the retained segment, or approximated ones, as they are or turned back with pairs (x[i], x[i + D / 2]) or
+// (x[2 i], x[2 i + 1]).
+enum class Fp4RowKind { kRetained, kApprox, kTurnedApart, kTurnedNext };
+
 // T: of the query, W, the output and the step's token.  SIDE: no more than eight query rows, T bf16.
-template <typename T, int D, bool SIDE, bool ROPE>
+template <typename T, int D, bool SIDE, Fp4RowKind KIND>
 __device__ __forceinline__ void attend_fp4(const Fp4Params& f, const RopeParams& rp, const SplitRows& range, int tid) {
   constexpr bool kExact = sizeof(T) == 4;              // fp32: query and weights in three parts, all their bits
   constexpr int kParts = kExact ? 3 : SIDE ? 1 : 2;    // of a weight, in products of their own
@@ -84,7 +91,6 @@ __device__ __forceinline__ void attend_fp4(const Fp4Params& f, const RopeParams&
   constexpr int NC = D / 32, NT = D / 16;              // score products per tile; tiles of the output dims
   constexpr int kCode = fp4_code_bytes(D), kScale = fp4_scale_bytes(D);
   constexpr int kRedStride = D + 4;
-  constexpr float kNegBig = -1.0e30f;                  // reference before any row: finite, so differences stay finite
   constexpr int kStepRows = DW * kFp4TileRows;
   typedef Fp4Stage<D> St;
 
@@ -93,7 +99,8 @@ __device__ __forceinline__ void attend_fp4(const Fp4Params& f, const RopeParams&
   const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int m = lane & 15, quarter = lane >> 4;
   const SegmentRows seg = range.seg;
-  const bool is_apx = range.is_apx, paged = !is_apx && seg.blocks != nullptr;
+  constexpr bool is_apx = KIND != Fp4RowKind::kRetained, apart = KIND == Fp4RowKind::kTurnedApart, turned = apart || KIND == Fp4RowKind::kTurnedNext;
+  const bool paged = !is_apx && seg.blocks != nullptr;
   const int row_begin = range.begin, row_end = range.end;
   const size_t bh = (size_t)range.b * p.Hkv + range.h;
   // rows in memory: the step's own token, the last live row, comes from the caller's tensors
@@ -123,10 +130,12 @@ __device__ __forceinline__ void attend_fp4(const Fp4Params& f, const RopeParams&
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
       if constexpr (!kExact) {
-        qf[0][c] = *reinterpret_cast<const u32x4*>(q + c * 8);
+        qf[0][c] = *reinterpret_cast<const u32x4*>(q + c * 8) ^ (f.flip | f.flip >> 16);
       } else {
         float x[8];
         load8(q + c * 8, x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(__float_as_uint(x[e]) ^ f.flip);
 #pragma unroll
         for (int part = 0; part < kQueryParts; ++part) {
           float y[8];
@@ -139,10 +148,13 @@ __device__ __forceinline__ void attend_fp4(const Fp4Params& f, const RopeParams&
     }
   }
 
-  f32x4 o[NT];
+  // The sum of a column's weights is one more row of the second product, of ones: the same in every lane, and of the weights as they
+  // went in.
+  f32x4 o[NT], o_sum = zero;
 #pragma unroll
   for (int j = 0; j < NT; ++j) o[j] = zero;
-  float ref = kNegBig, l_run = 0.f;
+  const u32x4 ones = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
+  float ref = -INFINITY;
 
   // paged: ids of the blocks from window on, one a lane
   int window = row_begin >> seg.block_shift, ids = 0;
@@ -160,14 +172,16 @@ __device__ __forceinline__ void attend_fp4(const Fp4Params& f, const RopeParams&
 
   extern __shared__ __align__(16) unsigned char fp4_lds[];
   unsigned char* ring = fp4_lds + wave * (kFp4Stages * St::kBytes);
-  const int32_t* positions = (ROPE && is_apx && rp.positions) ? rp.positions + seg.apx_row0 : nullptr;
-  const bool turned = ROPE && is_apx;
+  const int32_t* positions = (turned && rp.positions) ? rp.positions + seg.apx_row0 : nullptr;
   // what a lane brings in: a 16-byte piece of codes of one row (a load), and of one more kRowsPerLoad / 4 further on in every eight (the next
   // load); the scales of one row
   const int in_place = lane / St::kPieces, in_row = 8 * (in_place & 3) + (in_place >> 2);
   const int in_piece = (lane % St::kPieces) ^ St::twist(in_place);
   // (the second load's places are 16 further on, which the permutation does not see)
   const int scale_row = lane & 31;
+  const uint32_t in_code = in_row * kCode + in_piece * 16;
+  const uint8_t* in_scale = (lane < 32 ? k_scales : r_scales) + scale_row * kScale;
+  const bool small_blocks = paged && seg.block_shift < 5;
   bool holes = false;                                  // a block that does not exist has been met
 
   auto fill = [&](int base, unsigned char* st) VEC_INLINE {
@@ -184,16 +198,21 @@ __device__ __forceinline__ void attend_fp4(const Fp4Params& f, const RopeParams&
     }
     const uint32_t to = lds_address(st);
     if (base + kFp4TileRows <= stored && lo && hi) {   // uniform: rows that are all there
-      const int64_t row = (in_row < 16 ? at_lo : at_hi) + in_row;
-      const uint8_t* k = k_codes + row * kCode + in_piece * 16;
+      auto codes = [&](const uint8_t* from, int64_t at, uint32_t dst) VEC_INLINE {
 #pragma unroll
-      for (int i = 0; i < St::kLoads; ++i) load_to_lds16(to + i * 1024, k + i * (8 / St::kLoads) * kCode);
-      if (!is_apx) {
-        const uint8_t* r = r_codes + row * kCode + in_piece * 16;
-#pragma unroll
-        for (int i = 0; i < St::kLoads; ++i) load_to_lds16(to + St::kTensor + i * 1024, r + i * (8 / St::kLoads) * kCode);
+        for (int i = 0; i < St::kLoads; ++i) load_to_lds16(dst + i * 1024, from + (at + i * (8 / St::kLoads)) * kCode, in_code);
+      };
+      const void* s = in_scale + (small_blocks && scale_row >= 16 ? at_hi : at_lo) * kScale;
+      if (!small_blocks || is_apx) {
+        codes(k_codes, at_lo, to);
+        if (!is_apx) codes(r_codes, at_lo, to + St::kTensor);
+      } else if (in_row < 16) {                        // half of the lanes' rows lie in either block
+        codes(k_codes, at_lo, to);
+        codes(r_codes, at_lo, to + St::kTensor);
+      } else {
+        codes(k_codes, at_hi, to);
+        codes(r_codes, at_hi, to + St::kTensor);
       }
-      const void* s = (lane < 32 ? k_scales : r_scales) + ((scale_row < 16 ? at_lo : at_hi) + scale_row) * kScale;
       if (!turned) {
         if constexpr (D == 128) load_to_lds4(to + St::kSlots, s);
         else load_to_lds2(to + St::kSlots, s);
@@ -239,7 +258,7 @@ __device__ __forceinline__ void attend_fp4(const Fp4Params& f, const RopeParams&
       if (lane == 0) *reinterpret_cast<uint32_t*>(st + St::kAlive) = alive;
     }
     wave_fence();
-    if (new_row >= base && new_row < base + kFp4TileRows && lane < D / 4) {
+    if (!is_apx && new_row >= base && new_row < base + kFp4TileRows && lane < D / 4) {
       // eight elements of the token's key or value a lane, as vector_store_fp4 rounds them
       constexpr int kLanes = D / 8;
       const int t = lane / kLanes, i = lane % kLanes, row = new_row - base;
@@ -258,24 +277,26 @@ __device__ __forceinline__ void attend_fp4(const Fp4Params& f, const RopeParams&
 
   // a lane's rows of a tile in operand order: the key row (and that four further on), the first of the eight of R
   const int k_row = 8 * (m >> 2) + (m & 3), r_row = 8 * quarter;
-  const int my_block = m / (16 / kScale);
-
-  // under ROPE a lane's dims always belong to the same rotary pairs
+  // How a lane's dims of R lie: kDims consecutive ones, or (keys that are turned back with pairs (x[i], x[i + D / 2])) kDims / 2 and their
+  // partners.  A word of scale bytes is turned so that the byte of the lane's block is a float's exponent, which is all that the conversions
+  // look at (all bytes and codes compared with junk around the exponent).
   constexpr int kDims = D / 16;
-  float t_hi[ROPE ? kDims : 1], t_lo[ROPE ? kDims : 1];
-  if constexpr (ROPE) {
-    if (is_apx) {
+  const uint32_t to_exponent = 8u * (apart ? kDims / 2 * m / kFp4Block : kDims * m / kFp4Block) + 9u;
+  auto exponent = [](uint32_t bytes, uint32_t by) VEC_INLINE { return __uint_as_float(__builtin_amdgcn_alignbit(bytes, bytes, by)); };
+  const uint32_t half_mask = m >= 8 ? 0xffff0000u : 0u;
+
+  // a lane's dims always belong to the same kDims / 2 rotary pairs
+  float t_hi[turned ? kDims / 2 : 1], t_lo[turned ? kDims / 2 : 1];
+  if constexpr (turned) {
 #pragma unroll
-      for (int e = 0; e < kDims; ++e) {
-        const int dim = kDims * m + e, i = rp.interleaved ? dim / 2 : dim % (D / 2);
-        t_hi[e] = rp.turns_hi[i];
-        t_lo[e] = rp.turns_lo[i];
-      }
+    for (int e = 0; e < kDims / 2; ++e) {
+      t_hi[e] = rp.turns_hi[kDims / 2 * m + e];
+      t_lo[e] = rp.turns_lo[kDims / 2 * m + e];
     }
   }
+
   auto consume = [&](const unsigned char* st, int base) VEC_INLINE {
-    // scores, in the log2 domain
-    float s[8];
+    float s[8];                                        // scores; times d.c2 they are in the log2 domain
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const int row = k_row + 4 * u;
@@ -299,67 +320,84 @@ __device__ __forceinline__ void attend_fp4(const Fp4Params& f, const RopeParams&
         for (int part = 0; part < kQueryParts; ++part) acc = mfma(a, qf[part][c], acc);
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s[4 * u + i] = acc[i] * p.c2;
+      for (int i = 0; i < 4; ++i) s[4 * u + i] = acc[i];
     }
-    if (holes || base + kFp4TileRows > stored) {
-      const uint32_t alive = *reinterpret_cast<const uint32_t*>(st + St::kAlive) >> r_row;
+    const bool some_dead = holes || base + kFp4TileRows > stored;
+    uint32_t alive = 0;
+    if (some_dead) {
+      alive = *reinterpret_cast<const uint32_t*>(st + St::kAlive) >> r_row;
 #pragma unroll
       for (int j = 0; j < 8; ++j) s[j] = (alive >> j & 1) ? s[j] : -INFINITY;
     }
     float top = s[0];
 #pragma unroll
     for (int j = 1; j < 8; ++j) top = fmaxf(top, s[j]);
+    top *= p.c2;
     // The reference of a column is raised only where a score lies far above it: the weights are then at most 2^kRaiseAt, and a
     // sum of them does not leave the range of a float.  The same in all lanes of a column.
     if (__ballot(top > ref + kRaiseAt)) {
       top = fmaxf(top, __shfl_xor(top, 16, kWave));
       top = fmaxf(top, __shfl_xor(top, 32, kWave));
-      const float next = fmaxf(ref, top), by = fast_exp2(ref - next);
-      l_run *= by;
+      const float next = fmaxf(ref, top), by = ref == next ? 1.f : fast_exp2(ref - next);
+      o_sum *= by;
 #pragma unroll
-      for (int j = 0; j < NT; ++j)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) o[j][i] *= by;
+      for (int j = 0; j < NT; ++j) o[j] *= by;
       ref = next;
     }
     float w[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      w[j] = fast_exp2(s[j] - ref);
-      l_run += w[j];
+    for (int j = 0; j < 8; ++j) w[j] = fast_exp2(fmaf(s[j], p.c2, -ref));
+    if (some_dead) {                                   // no row yet: minus infinity less itself
+#pragma unroll
+      for (int j = 0; j < 8; ++j) w[j] = (alive >> j & 1) ? w[j] : 0.f;
     }
     u32x4 weights[kParts];
 #pragma unroll
     for (int part = 0; part < kParts; ++part) {
-      float y[8];
+      if constexpr (SIDE) {                            // columns from 8 on: what is left of the weight
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        y[j] = leading(w[j]);
-        if constexpr (SIDE) { if (m >= 8) y[j] = w[j] - y[j]; }
-        else w[j] -= y[j];
+        for (int j = 0; j < 8; ++j) w[j] -= __uint_as_float(__float_as_uint(w[j]) & half_mask);
       }
-      // what SIDE leaves has up to 16 bits and is rounded to the nearest eight; the others are cut exactly
 #pragma unroll
-      for (int i = 0; i < 4; ++i) weights[part][i] = SIDE ? pack_bf16(y[2 * i], y[2 * i + 1]) : high_halves(y[2 * i], y[2 * i + 1]);
+      for (int i = 0; i < 4; ++i) weights[part][i] = high_halves(w[2 * i], w[2 * i + 1]);
+      if (part + 1 < kParts) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] -= leading(w[j]);
+      }
+      o_sum = mfma(ones, weights[part], o_sum);
     }
-    // the eight rows of R, and their scales for the lane's dims
-    uint32_t r[8];
-    float unit[8];
+    // the eight rows of R, and their scale bytes
+    uint32_t r[8], bytes[8];
     const unsigned char* rt = st + (is_apx ? 0 : St::kTensor);
     const unsigned char* slots = st + St::kSlots + (is_apx ? 0 : 128);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const int at = St::piece(r_row + j, D == 128 ? m >> 2 : m >> 3);
-      if constexpr (D == 128) r[j] = *reinterpret_cast<const uint32_t*>(rt + at + (m & 3) * 4);
-      else r[j] = *reinterpret_cast<const uint16_t*>(rt + at + (m & 7) * 2);
+      // row 8 quarter + j, the (4 j + quarter)-th; x: how its pieces are permuted
+      const int x = St::twist(4 * j), at = 4 * j * kCode;
+      if constexpr (!apart) {
+        const unsigned char* from = rt + quarter * kCode + at;
+        if constexpr (D == 128) r[j] = *reinterpret_cast<const uint32_t*>(from + (((m >> 2) ^ x) * 16 + (m & 3) * 4));
+        else r[j] = *reinterpret_cast<const uint16_t*>(from + (((m >> 3) ^ x) * 16 + (m & 7) * 2));
+      } else {                                         // dims kDims / 2 m .. in the low half, their partners, half a row on, in the high one
+        const unsigned char* from = rt + quarter * kCode + at;
+        if constexpr (D == 128) {
+          r[j] = (uint32_t)*reinterpret_cast<const uint16_t*>(from + (((m >> 3) ^ x) * 16 + (m & 7) * 2)) |
+                 (uint32_t)*reinterpret_cast<const uint16_t*>(from + (((m >> 3) ^ x ^ 2) * 16 + (m & 7) * 2)) << 16;
+        } else {
+          r[j] = (uint32_t)from[x * 16 + m] | (uint32_t)from[(x ^ 1) * 16 + m] << 16;
+        }
+      }
     }
 #pragma unroll
     for (int j = 0; j < 8; j += 4) {
       const u32x4 x = *reinterpret_cast<const u32x4*>(slots + (r_row + j) * 4);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) unit[j + i] = fp4_unit(x[i] >> 8 * my_block & 0xffu);
+      for (int i = 0; i < 4; ++i) bytes[j + i] = x[i];
     }
-    if (!ROPE || !is_apx) {
+    if constexpr (!turned) {
+      float unit[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) unit[j] = exponent(bytes[j], to_exponent);
       for_each_constant<kDims / 2>([&](auto c) VEC_INLINE {
         uint32_t two[8];
 #pragma unroll
@@ -376,62 +414,69 @@ __device__ __forceinline__ void attend_fp4(const Fp4Params& f, const RopeParams&
           o[2 * c + 1] = mfma(odd, weights[part], o[2 * c + 1]);
         }
       });
-      return;
-    }
-    if constexpr (ROPE) {
+    } else {
       // keys turned back, in one bf16 part (three for fp32): they carry that one rounding, as those of a bf16 cache do
       constexpr int kRowParts = kExact ? 3 : 1;
       float pos[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) pos[j] = (float)(*reinterpret_cast<const int*>(st + St::kPositions + (r_row + j) * 4) + rp.pos_offset);
-      for_each_constant<kDims / 2>([&](auto c) VEC_INLINE {
-        f32x2 two[8];
+      auto add = [&](f32x4& sum, float* x) VEC_INLINE {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          f32x2 x = fp4_pair_f32<decltype(c)::value>(r[j], unit[j]);
-          if (rp.interleaved) {
-            float cs, sn;
-            rotary_cos_sin(pos[j], t_hi[2 * c], t_lo[2 * c], cs, sn);
-            float a, b;
-            rotary_back(x[0], x[1], cs, sn, a, b);
-            x[0] = a;
-            x[1] = b;
-          } else {
-            // pairs (x[i], x[i + D / 2]): the other member is in the lane eight further on or back
+        for (int rest = 0; rest < kRowParts; ++rest) {
+          u32x4 a;
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
+          for (int i = 0; i < 4; ++i) a[i] = kRowParts == 1 ? pack_bf16(x[2 * i], x[2 * i + 1]) : high_halves(x[2 * i], x[2 * i + 1]);
+          if (rest + 1 < kRowParts) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] -= leading(x[j]);
+          }
+#pragma unroll
+          for (int part = 0; part + rest < kParts; ++part) sum = mfma(a, weights[part], sum);
+        }
+      };
+      if constexpr (apart) {
+        constexpr int kHalf = kDims / 2;               // pairs of a lane, two a byte of codes
+        for_each_constant<kHalf / 2>([&](auto c) VEC_INLINE {
+          f32x2 x[8], y[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            x[j] = fp4_pair_f32<decltype(c)::value>(r[j], exponent(bytes[j], to_exponent));
+            y[j] = fp4_pair_f32<2 + decltype(c)::value>(r[j], exponent(bytes[j], to_exponent + kScale / 2 * 8u));
+          }
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            float a[8], b[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
               float cs, sn;
               rotary_cos_sin(pos[j], t_hi[2 * c + e], t_lo[2 * c + e], cs, sn);
-              const float other = __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x[e]), 0x128, 0xf, 0xf, false));   // row_ror:8
-              x[e] = m < 8 ? fmaf(x[e], cs, other * sn) : fmaf(x[e], cs, -(other * sn));
+              rotary_back(x[j][e], y[j][e], cs, sn, a[j], b[j]);
             }
+            add(o[2 * c + e], a);
+            add(o[kHalf + 2 * c + e], b);
+            __builtin_amdgcn_sched_barrier(0);         // all pairs' sines at once would not fit the registers
           }
-          two[j] = x;
-        }
+        });
+      } else {
+        for_each_constant<kDims / 2>([&](auto c) VEC_INLINE {
+          float a[8], b[8];
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
-#pragma unroll
-          for (int rest = 0; rest < kRowParts; ++rest) {
-            u32x4 a;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              if constexpr (kRowParts == 1) {
-                a[i] = pack_bf16(two[2 * i][e], two[2 * i + 1][e]);
-              } else {
-                a[i] = high_halves(two[2 * i][e], two[2 * i + 1][e]);
-                two[2 * i][e] -= leading(two[2 * i][e]);
-                two[2 * i + 1][e] -= leading(two[2 * i + 1][e]);
-              }
-            }
-#pragma unroll
-            for (int part = 0; part + rest < kParts; ++part) o[2 * c + e] = mfma(a, weights[part], o[2 * c + e]);
+          for (int j = 0; j < 8; ++j) {
+            const f32x2 x = fp4_pair_f32<decltype(c)::value>(r[j], exponent(bytes[j], to_exponent));
+            float cs, sn;
+            rotary_cos_sin(pos[j], t_hi[c], t_lo[c], cs, sn);
+            rotary_back(x[0], x[1], cs, sn, a[j], b[j]);
           }
-      });
+          add(o[2 * c], a);
+          add(o[2 * c + 1], b);
+          __builtin_amdgcn_sched_barrier(0);
+        });
+      }
     }
   };
 
   // loads of a tile; of tiles that went by the other way there are none on their way, nor of any before these
-  const int per_tile = is_apx ? St::kLoads + 1 + (D == 64 && turned && positions ? 1 : 0) : 2 * St::kLoads + 1;
+  const int per_tile = is_apx ? St::kLoads + 1 + (D == 64 && turned && positions ? 1 : 0) : (small_blocks ? 4 : 2) * St::kLoads + 1;
   static_assert(kFp4Stages == 3, "two tiles on their way while one is worked on");
   const int tiles = row_begin + wave * kFp4TileRows < row_end ? (row_end - row_begin - wave * kFp4TileRows + kStepRows - 1) / kStepRows : 0;
   const int first = row_begin + wave * kFp4TileRows;
@@ -461,17 +506,18 @@ __device__ __forceinline__ void attend_fp4(const Fp4Params& f, const RopeParams&
   auto red = [&](int wv, int col, int j) VEC_INLINE { return reinterpret_cast<float*>(fp4_lds + wv * kWaveBytes) + col * kRedStride + j; };
   auto ml = [&](int wv, int what, int col) VEC_INLINE { return reinterpret_cast<float*>(fp4_lds + wv * kWaveBytes) + 16 * kRedStride + what * 16 + col; };
   wave_fence();
-  float l_tot = l_run + __shfl_xor(l_run, 16, kWave);
-  l_tot += __shfl_xor(l_tot, 32, kWave);
-  // lane (m, quarter): column m, dims kDims * (4 quarter + i) + j
+  // lane (m, quarter): column m, dims of lane 4 quarter + i
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int j = 0; j < NT; j += 4)
-      *reinterpret_cast<f32x4*>(red(wave, m, kDims * (4 * quarter + i) + j)) = f32x4{o[j][i], o[j + 1][i], o[j + 2][i], o[j + 3][i]};
+    for (int j = 0; j < NT; j += kDims / 2) {
+      const int dim = apart ? j / (kDims / 2) * (D / 2) + kDims / 2 * (4 * quarter + i) : kDims * (4 * quarter + i) + j;
+#pragma unroll
+      for (int e = 0; e < kDims / 2; e += 2) *reinterpret_cast<f32x2*>(red(wave, m, dim + e)) = f32x2{o[j + e][i], o[j + e + 1][i]};
+    }
   if (quarter == 0) {
-    *ml(wave, 0, m) = l_tot > 0.f ? ref : -INFINITY;    // a wave without rows: its share is 0 without a branch
-    *ml(wave, 1, m) = l_tot;
+    *ml(wave, 0, m) = ref;                             // minus infinity of a wave without rows: its share is 0 without a branch
+    *ml(wave, 1, m) = o_sum[0];
   }
   __syncthreads();
   float* out = p.part + range.slot * PSZ;
@@ -489,7 +535,7 @@ __device__ __forceinline__ void attend_fp4(const Fp4Params& f, const RopeParams&
       if constexpr (SIDE) x += *reinterpret_cast<const f32x4*>(red(wv, 8 + g, j));
 #pragma unroll
       for (int e = 0; e < 4; ++e) a[e] = fmaf(x[e], sc, a[e]);
-      l = fmaf(*ml(wv, 1, g), sc, l);
+      l = fmaf(SIDE ? *ml(wv, 1, g) + *ml(wv, 1, 8 + g) : *ml(wv, 1, g), sc, l);
     }
     *reinterpret_cast<f32x4_u*>(out + 2 * G + i) = a;
     if (j == 0) {
@@ -499,30 +545,37 @@ __device__ __forceinline__ void attend_fp4(const Fp4Params& f, const RopeParams&
   }
 }
 
-template <typename T, int D, bool SIDE, bool ROPE>
+template <typename T, int D, bool SIDE, Fp4RowKind APPROX>
 __global__ __launch_bounds__(DT_, 3) void decode_split_fp4_kernel(Fp4Params f, RopeParams rp) {
-  attend_fp4<T, D, SIDE, ROPE>(f, rp, grid_split<DW * kFp4TileRows>(f.d), (int)threadIdx.x);
+  const SplitRows r = grid_split<DW * kFp4TileRows>(f.d);
+  if (r.is_apx) attend_fp4<T, D, SIDE, APPROX>(f, rp, r, (int)threadIdx.x);
+  else attend_fp4<T, D, SIDE, Fp4RowKind::kRetained>(f, rp, r, (int)threadIdx.x);
 }
 
-template <typename T, int D, bool SIDE, bool ROPE>
+template <typename T, int D, bool SIDE, Fp4RowKind APPROX>
 int launch_split_fp4(const Fp4Params& f, const RopeParams* rope, hipStream_t stream) {
   const dim3 grid(f.d.splits_ret + f.d.splits_apx, f.d.Hkv, f.d.B);
   constexpr int lds = DW * kFp4Stages * Fp4Stage<D>::kBytes;
-  VEC_HIP(set_max_lds(reinterpret_cast<const void*>(decode_split_fp4_kernel<T, D, SIDE, ROPE>), lds));
-  VEC_LAUNCH(K_DECODE_SPLIT, (decode_split_fp4_kernel<T, D, SIDE, ROPE>), grid, dim3(DT_), lds, stream, f, rope ? *rope : RopeParams{});
+  VEC_HIP(set_max_lds(reinterpret_cast<const void*>(decode_split_fp4_kernel<T, D, SIDE, APPROX>), lds));
+  VEC_LAUNCH(K_DECODE_SPLIT, (decode_split_fp4_kernel<T, D, SIDE, APPROX>), grid, dim3(DT_), lds, stream, f, rope ? *rope : RopeParams{});
   VEC_HIP(hipGetLastError());
   return VECTOR_OK;
 }
 
-template <typename T, int D>
+template <typename T, int D, bool SIDE>
 int run_split_fp4(Fp4Params& f, const RopeParams* rope, hipStream_t stream) {
   pick_splits_fp4(f.d.B, f.d.Hkv, f.d.cap_retain, f.d.n_approx, f.d.splits_ret, f.d.splits_apx);
-  const bool turned = rope && f.d.n_approx > 0;
+  if (!rope || f.d.n_approx == 0) return launch_split_fp4<T, D, SIDE, Fp4RowKind::kApprox>(f, nullptr, stream);
+  return rope->interleaved ? launch_split_fp4<T, D, SIDE, Fp4RowKind::kTurnedNext>(f, rope, stream)
+                           : launch_split_fp4<T, D, SIDE, Fp4RowKind::kTurnedApart>(f, rope, stream);
+}
+
+template <typename T, int D>
+int run_fp4(Fp4Params& f, const RopeParams* rope, hipStream_t stream) {
   if constexpr (sizeof(T) == 2) {
-    if (f.d.Hq / f.d.Hkv <= 8)
-      return turned ? launch_split_fp4<T, D, true, true>(f, rope, stream) : launch_split_fp4<T, D, true, false>(f, rope, stream);
+    if (f.d.Hq / f.d.Hkv <= 8) return run_split_fp4<T, D, true>(f, rope, stream);
   }
-  return turned ? launch_split_fp4<T, D, false, true>(f, rope, stream) : launch_split_fp4<T, D, false, false>(f, rope, stream);
+  return run_split_fp4<T, D, false>(f, rope, stream);
 }
 
 }  // namespace
@@ -541,12 +594,15 @@ int launch_decode_fp4(const vector_cache_fp4& c, const void* q, float scale, voi
   p.out = out; p.part = reinterpret_cast<float*>(ws);
   p.B = c.batch; p.Hq = c.n_q_heads; p.Hkv = c.n_kv_heads; p.cap_retain = c.cap_retain; p.n_approx = c.n_approx;
   p.w_sh = c.w_shared ? 0 : (int64_t)c.head_dim * c.head_dim;
-  p.c2 = scale * kLog2e;
+  // (the least number for a scale of 0: times a score that is 0 in the log2 domain as well, times minus infinity it is what masks a row)
+  const float c2 = scale * kLog2e;
+  p.c2 = fmaxf(fabsf(c2), 1.17549435e-38f);
+  f.flip = c2 < 0.f ? 0x80000000u : 0u;
   f.k_ret_scale = c.k_ret_scale; f.v_ret_scale = c.v_ret_scale; f.k_apx_scale = c.k_apx_scale;
   f.n_blocks = c.n_blocks;
   int rc;
-  if (c.dtype == VECTOR_BF16) rc = c.head_dim == 128 ? run_split_fp4<bf16_t, 128>(f, rope, stream) : run_split_fp4<bf16_t, 64>(f, rope, stream);
-  else rc = c.head_dim == 128 ? run_split_fp4<float, 128>(f, rope, stream) : run_split_fp4<float, 64>(f, rope, stream);
+  if (c.dtype == VECTOR_BF16) rc = c.head_dim == 128 ? run_fp4<bf16_t, 128>(f, rope, stream) : run_fp4<bf16_t, 64>(f, rope, stream);
+  else rc = c.head_dim == 128 ? run_fp4<float, 128>(f, rope, stream) : run_fp4<float, 64>(f, rope, stream);
   return rc ? rc : launch_decode_merge(p, c.dtype, c.head_dim, stream);
 }
 
