@@ -3,23 +3,26 @@
 // partial results and the same merge.
 //
 // What bounds it is memory, 136 bytes for the key and the value of a token at 128 dims, against 512 in bf16; but a quarter of the bytes
-// leaves a quarter of the time for a row's arithmetic.  Both products run on the matrix cores in bf16 with fp32 sums:
-// an element in 4 bits times its scale has two significant bits and is a bf16 number exactly, so the only
-// roundings are those of the weights, which go in as parts of eight bits each (kParts).
+// leaves a quarter of the time for a row's arithmetic, which comes close behind it.  Both products run on the matrix cores with fp32 sums.
+// An element in 4 bits times its scale has two significant bits and is a bf16 number exactly; the weights go in as parts of eight bits each.
 //
 // A wave takes 32 rows at a time and waits for no other before the end.  Their codes and scales go from memory straight into a ring of its
 // own in LDS (Fp4Stage), so that what is on its way takes no registers, and are read back in the matrix cores' order:
 //   scores   S[t][g] = sum_e K[t][e] q[g][e]      A = K: lane (m, quarter) holds D / 4 consecutive elements of a row, which is one read and
-//                                                  one scale; B = the query rows in the same order of e
+//                                                  one scale.  128 dims: as they are, in 4 bits with their scales, against query rows in
+//                                                  two fp8 parts (kMx); 64 dims and fp32: converted to bf16
 //   output   O[j][g] += sum_t R[t][j] P[t][g]     A = R^T: lane (m, quarter) holds dims D / 16 m .. of eight rows, 8 quarter ..; the conversion
-//                                                  hands out two neighbouring dims of one row, and a byte permutation makes
-//                                                  two rows of one dim of them
+//                                                  hands out two neighbouring dims of one row
 // Row 4 a + i of score tile u is token 8 a + 4 u + i, so that the eight weights that a lane gets from both score tiles are those
 // of the eight rows that it holds of R.  R is the values, or for approximated rows the keys, read a second time in the other order;
 // under ROPE these are turned back by their positions first.
 //
-// Sixteen columns hold up to 16 query rows.  Up to eight (SIDE): columns g take the weights' leading bits and columns 8 + g what these leave,
-// with one product for both.
+// Sixteen columns, COLS of them for different query rows:
+//   4   columns 4 and 12 on take what the weights' leading bits leave.  The contraction runs over (row, even or odd dim), as the conversion hands
+//       them out; the weights of columns below 8 are zero at odd dims, those from 8 on at even ones, so that a product gives both dims,
+//       each in columns of its own, and half of the sums' registers are enough
+//   8   columns from 8 on take what the leading bits leave; a byte permutation makes two rows of one dim of two dims of one row
+//   16  leading bits and the rest in products of their own
 #include "decode_split.hpp"
 #include "fp4.hpp"
 #include "launch.hpp"
@@ -82,15 +85,18 @@ constexpr int kFp4Stages = 3;
 // (x[2 i], x[2 i + 1]).
 enum class Fp4RowKind { kRetained, kApprox, kTurnedApart, kTurnedNext };
 
-// T: of the query, W, the output and the step's token.  SIDE: no more than eight query rows, T bf16.
-template <typename T, int D, bool SIDE, Fp4RowKind KIND>
+// T: of the query, W, the output and the step's token.  COLS: no fewer than the query rows; 16 for fp32.
+template <typename T, int D, int COLS, Fp4RowKind KIND>
 __device__ __forceinline__ void attend_fp4(const Fp4Params& f, const RopeParams& rp, const SplitRows& range, int tid) {
   constexpr bool kExact = sizeof(T) == 4;              // fp32: query and weights in three parts, all their bits
-  constexpr int kParts = kExact ? 3 : SIDE ? 1 : 2;    // of a weight, in products of their own
-  constexpr int kQueryParts = kExact ? 3 : 1;
-  constexpr int NC = D / 32, NT = D / 16;              // score products per tile; tiles of the output dims
+  constexpr bool kMx = D == 128 && !kExact;            // scores from the codes
+  constexpr bool kQuad = COLS == 4, kSide = COLS == 8;
+  static_assert(!kExact || COLS == 16, "parts in products of their own");
+  constexpr int kParts = kExact ? 3 : COLS == 16 ? 2 : 1;        // of a weight, in products of their own
+  constexpr int kQueryParts = kExact ? 3 : kMx && COLS == 16 ? 2 : 1;
+  constexpr int NC = D / 32, NT = kQuad ? D / 32 : D / 16;       // score products per tile; tiles of the output dims
   constexpr int kCode = fp4_code_bytes(D), kScale = fp4_scale_bytes(D);
-  constexpr int kRedStride = D + 4;
+  constexpr int kRedStride = (kQuad ? D / 2 : D) + 4;  // floats of a column, in kQuad of every other dim
   constexpr int kStepRows = DW * kFp4TileRows;
   typedef Fp4Stage<D> St;
 
@@ -122,18 +128,65 @@ __device__ __forceinline__ void attend_fp4(const Fp4Params& f, const RopeParams&
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
   };
 
-  // query rows: column m holds row m, or m % 8
-  u32x4 qf[kQueryParts][NC];
-  {
-    const int g = min(SIDE ? m & 7 : m, G - 1);
-    const T* q = reinterpret_cast<const T*>(p.q) + ((size_t)range.b * p.Hq + (size_t)range.h * G + g) * D + quarter * (D / 4);
+  // query rows: column m holds row m % COLS; the rest of a weight (lo) belongs to it in some columns
+  const bool lo = kQuad ? m & 4 : kSide ? m & 8 : false;
+  const T* q_row = reinterpret_cast<const T*>(p.q) + ((size_t)range.b * p.Hq + (size_t)range.h * G + min(m & (COLS - 1), G - 1)) * D;
+  u32x4 qf[kMx ? 1 : kQueryParts][kMx ? 1 : NC];
+  i32x8 qx[kMx ? kQueryParts : 1];
+  int q_unit[kMx ? kQueryParts : 1];
+  if constexpr (kMx) {
+    // A row in two fp8 parts under a scale for every 32 dims: four bits and the four behind them, all that bf16 has; an element far below its
+    // block's largest is off by 2^-22 of that at most.  The matrix core takes 16 dims from 16 quarter on and 16 from 64 + 16 quarter
+    // on from a lane, and the scale of dims 32 quarter .. (compared with one-hot operands); a block's dims are in two lanes.
+    float x[2][16];
+    int top[2];
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      load8(q_row + half * 64 + quarter * 16, x[half]);
+      load8(q_row + half * 64 + quarter * 16 + 8, x[half] + 8);
+      uint32_t most = max(top_bits8(x[half]), top_bits8(x[half] + 8));
+      most = max(most, (uint32_t)__shfl_xor((int)most, 16, kWave));
+      // the largest between 128 and 256 units; an infinite or NaN element: NaN, in the whole block
+      top[half] = most >= 0x7f800000u ? 255 : min(max((int)(most >> 23) - 7, 6), 254);
+    }
+    const int first = __shfl(top[0], m + (quarter & 1) * 32, kWave), second = __shfl(top[1], m + (quarter & 1) * 32, kWave);
+    const int own = quarter < 2 ? first : second;      // of block `quarter`
+#pragma unroll
+    for (int part = 0; part < kQueryParts; ++part) q_unit[part] = own == 255 ? 255 : own - (lo || part == 1 ? 5 : 0);
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const int byte = top[half] == 255 ? 127 : top[half];
+      const float unit = fp4_unit((uint32_t)byte), small = fp4_unit((uint32_t)(byte - 5));
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        s16x2 hi = {0, 0}, rest = {0, 0};
+        float y[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = __uint_as_float(__float_as_uint(x[half][4 * w + e]) ^ f.flip);
+        hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(hi, y[0], y[1], unit, false);
+        hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(hi, y[2], y[3], unit, true);
+        const int word = __builtin_bit_cast(int, hi);
+        const f32x2 back0 = __builtin_bit_cast(f32x2, __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(word, unit, false));
+        const f32x2 back1 = __builtin_bit_cast(f32x2, __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(word, unit, true));
+        rest = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(rest, y[0] - back0[0], y[1] - back0[1], small, false);
+        rest = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(rest, y[2] - back1[0], y[3] - back1[1], small, true);
+        if constexpr (kQueryParts == 2) {
+          qx[0][half * 4 + w] = word;
+          qx[1][half * 4 + w] = __builtin_bit_cast(int, rest);
+        } else {
+          qx[0][half * 4 + w] = lo ? __builtin_bit_cast(int, rest) : word;
+        }
+      }
+    }
+  } else {
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
+      const T* q = q_row + quarter * (D / 4) + c * 8;
       if constexpr (!kExact) {
-        qf[0][c] = *reinterpret_cast<const u32x4*>(q + c * 8) ^ (f.flip | f.flip >> 16);
+        qf[0][c] = *reinterpret_cast<const u32x4*>(q) ^ (f.flip | f.flip >> 16);
       } else {
         float x[8];
-        load8(q + c * 8, x);
+        load8(q, x);
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(__float_as_uint(x[e]) ^ f.flip);
 #pragma unroll
@@ -283,7 +336,8 @@ __device__ __forceinline__ void attend_fp4(const Fp4Params& f, const RopeParams&
   constexpr int kDims = D / 16;
   const uint32_t to_exponent = 8u * (apart ? kDims / 2 * m / kFp4Block : kDims * m / kFp4Block) + 9u;
   auto exponent = [](uint32_t bytes, uint32_t by) VEC_INLINE { return __uint_as_float(__builtin_amdgcn_alignbit(bytes, bytes, by)); };
-  const uint32_t half_mask = m >= 8 ? 0xffff0000u : 0u;
+  const uint32_t rest_mask = lo ? 0xffff0000u : 0u;
+  const uint32_t at_dim = m < 8 ? 0x0c0c0706u : 0x07060c0cu;        // kQuad: a weight's leading half in the low or the high half of a word
 
   // a lane's dims always belong to the same kDims / 2 rotary pairs
   float t_hi[turned ? kDims / 2 : 1], t_lo[turned ? kDims / 2 : 1];
@@ -310,14 +364,27 @@ __device__ __forceinline__ void attend_fp4(const Fp4Params& f, const RopeParams&
 #pragma unroll
         for (int c = 0; c < NC; ++c) words[c] = x[c];
       }
-      const float unit = fp4_unit(st[St::kSlots + row * 4 + (D == 128 ? quarter : quarter >> 1)]);
+      const uint32_t byte = st[St::kSlots + row * 4 + (D == 128 ? quarter : quarter >> 1)];
       f32x4 acc = zero;
+      if constexpr (kMx) {
+        const i32x8 a = {(int)words[0], (int)words[1], (int)words[2], (int)words[3], 0, 0, 0, 0};
 #pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        const uint32_t w = words[c];
-        const u32x4 a = {fp4_pair_bf16<0>(w, unit), fp4_pair_bf16<1>(w, unit), fp4_pair_bf16<2>(w, unit), fp4_pair_bf16<3>(w, unit)};
+        for (int part = 0; part < kQueryParts; ++part)
+          acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, qx[part], acc, 4, 0, 0, (int)byte, 0, q_unit[part]);
+        if constexpr (kQueryParts == 1) {              // the other part is in the columns COLS further on or back
 #pragma unroll
-        for (int part = 0; part < kQueryParts; ++part) acc = mfma(a, qf[part][c], acc);
+          for (int i = 0; i < 4; ++i)
+            acc[i] += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(acc[i]), 0x120 + COLS, 0xf, 0xf, false));
+        }
+      } else {
+        const float unit = fp4_unit(byte);
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          const uint32_t w = words[c];
+          const u32x4 a = {fp4_pair_bf16<0>(w, unit), fp4_pair_bf16<1>(w, unit), fp4_pair_bf16<2>(w, unit), fp4_pair_bf16<3>(w, unit)};
+#pragma unroll
+          for (int part = 0; part < kQueryParts; ++part) acc = mfma(a, qf[part][c], acc);
+        }
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) s[4 * u + i] = acc[i];
@@ -351,20 +418,28 @@ __device__ __forceinline__ void attend_fp4(const Fp4Params& f, const RopeParams&
 #pragma unroll
       for (int j = 0; j < 8; ++j) w[j] = (alive >> j & 1) ? w[j] : 0.f;
     }
-    u32x4 weights[kParts];
+    // kQuad: rows 0 .. 3 and 4 .. 7
+    u32x4 weights[kQuad ? 2 : kParts];
+    if constexpr (COLS != 16) {                        // columns of the rest
 #pragma unroll
-    for (int part = 0; part < kParts; ++part) {
-      if constexpr (SIDE) {                            // columns from 8 on: what is left of the weight
+      for (int j = 0; j < 8; ++j) w[j] -= __uint_as_float(__float_as_uint(w[j]) & rest_mask);
+    }
+    if constexpr (kQuad) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) w[j] -= __uint_as_float(__float_as_uint(w[j]) & half_mask);
+      for (int j = 0; j < 8; ++j) weights[j / 4][j % 4] = __builtin_amdgcn_perm(__float_as_uint(w[j]), __float_as_uint(w[j]), at_dim);
+      o_sum = mfma(ones, weights[0], o_sum);
+      o_sum = mfma(ones, weights[1], o_sum);
+    } else {
+#pragma unroll
+      for (int part = 0; part < kParts; ++part) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) weights[part][i] = high_halves(w[2 * i], w[2 * i + 1]);
+        if (part + 1 < kParts) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) w[j] -= leading(w[j]);
+        }
+        o_sum = mfma(ones, weights[part], o_sum);
       }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) weights[part][i] = high_halves(w[2 * i], w[2 * i + 1]);
-      if (part + 1 < kParts) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) w[j] -= leading(w[j]);
-      }
-      o_sum = mfma(ones, weights[part], o_sum);
     }
     // the eight rows of R, and their scale bytes
     uint32_t r[8], bytes[8];
@@ -402,16 +477,21 @@ __device__ __forceinline__ void attend_fp4(const Fp4Params& f, const RopeParams&
         uint32_t two[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) two[j] = fp4_pair_bf16<decltype(c)::value>(r[j], unit[j]);
-        u32x4 even, odd;
+        if constexpr (kQuad) {
+          o[c] = mfma(u32x4{two[0], two[1], two[2], two[3]}, weights[0], o[c]);
+          o[c] = mfma(u32x4{two[4], two[5], two[6], two[7]}, weights[1], o[c]);
+        } else {
+          u32x4 even, odd;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          even[i] = __builtin_amdgcn_perm(two[2 * i + 1], two[2 * i], 0x05040100u);
-          odd[i] = __builtin_amdgcn_perm(two[2 * i + 1], two[2 * i], 0x07060302u);
-        }
+          for (int i = 0; i < 4; ++i) {
+            even[i] = __builtin_amdgcn_perm(two[2 * i + 1], two[2 * i], 0x05040100u);
+            odd[i] = __builtin_amdgcn_perm(two[2 * i + 1], two[2 * i], 0x07060302u);
+          }
 #pragma unroll
-        for (int part = 0; part < kParts; ++part) {
-          o[2 * c] = mfma(even, weights[part], o[2 * c]);
-          o[2 * c + 1] = mfma(odd, weights[part], o[2 * c + 1]);
+          for (int part = 0; part < kParts; ++part) {
+            o[2 * c] = mfma(even, weights[part], o[2 * c]);
+            o[2 * c + 1] = mfma(odd, weights[part], o[2 * c + 1]);
+          }
         }
       });
     } else {
@@ -420,42 +500,53 @@ __device__ __forceinline__ void attend_fp4(const Fp4Params& f, const RopeParams&
       float pos[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) pos[j] = (float)(*reinterpret_cast<const int*>(st + St::kPositions + (r_row + j) * 4) + rp.pos_offset);
-      auto add = [&](f32x4& sum, float* x) VEC_INLINE {
+      // dims 2 t and 2 t + 1 of the lane's, of the eight rows
+      auto add = [&](auto t, float* even, float* odd) VEC_INLINE {
+        if constexpr (kQuad) {
 #pragma unroll
-        for (int rest = 0; rest < kRowParts; ++rest) {
-          u32x4 a;
+          for (int i = 0; i < 2; ++i) {
+            u32x4 a;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) a[i] = kRowParts == 1 ? pack_bf16(x[2 * i], x[2 * i + 1]) : high_halves(x[2 * i], x[2 * i + 1]);
-          if (rest + 1 < kRowParts) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] -= leading(x[j]);
+            for (int j = 0; j < 4; ++j) a[j] = pack_bf16(even[4 * i + j], odd[4 * i + j]);
+            o[t] = mfma(a, weights[i], o[t]);
           }
+        } else {
 #pragma unroll
-          for (int part = 0; part + rest < kParts; ++part) sum = mfma(a, weights[part], sum);
+          for (int e = 0; e < 2; ++e) {
+            float* x = e ? odd : even;
+#pragma unroll
+            for (int rest = 0; rest < kRowParts; ++rest) {
+              u32x4 a;
+#pragma unroll
+              for (int i = 0; i < 4; ++i) a[i] = kRowParts == 1 ? pack_bf16(x[2 * i], x[2 * i + 1]) : high_halves(x[2 * i], x[2 * i + 1]);
+              if (rest + 1 < kRowParts) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[j] -= leading(x[j]);
+              }
+#pragma unroll
+              for (int part = 0; part + rest < kParts; ++part) o[2 * t + e] = mfma(a, weights[part], o[2 * t + e]);
+            }
+          }
         }
+        __builtin_amdgcn_sched_barrier(0);             // all pairs' sines at once would not fit the registers
       };
       if constexpr (apart) {
         constexpr int kHalf = kDims / 2;               // pairs of a lane, two a byte of codes
         for_each_constant<kHalf / 2>([&](auto c) VEC_INLINE {
-          f32x2 x[8], y[8];
+          float a[2][8], b[2][8];
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
-            x[j] = fp4_pair_f32<decltype(c)::value>(r[j], exponent(bytes[j], to_exponent));
-            y[j] = fp4_pair_f32<2 + decltype(c)::value>(r[j], exponent(bytes[j], to_exponent + kScale / 2 * 8u));
-          }
+            const f32x2 x = fp4_pair_f32<decltype(c)::value>(r[j], exponent(bytes[j], to_exponent));
+            const f32x2 y = fp4_pair_f32<2 + decltype(c)::value>(r[j], exponent(bytes[j], to_exponent + kScale / 2 * 8u));
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            float a[8], b[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
+            for (int e = 0; e < 2; ++e) {
               float cs, sn;
               rotary_cos_sin(pos[j], t_hi[2 * c + e], t_lo[2 * c + e], cs, sn);
-              rotary_back(x[j][e], y[j][e], cs, sn, a[j], b[j]);
+              rotary_back(x[e], y[e], cs, sn, a[e][j], b[e][j]);
             }
-            add(o[2 * c + e], a);
-            add(o[kHalf + 2 * c + e], b);
-            __builtin_amdgcn_sched_barrier(0);         // all pairs' sines at once would not fit the registers
           }
+          add(std::integral_constant<int, decltype(c)::value>{}, a[0], a[1]);
+          add(std::integral_constant<int, kHalf / 2 + decltype(c)::value>{}, b[0], b[1]);
         });
       } else {
         for_each_constant<kDims / 2>([&](auto c) VEC_INLINE {
@@ -467,9 +558,7 @@ __device__ __forceinline__ void attend_fp4(const Fp4Params& f, const RopeParams&
             rotary_cos_sin(pos[j], t_hi[c], t_lo[c], cs, sn);
             rotary_back(x[0], x[1], cs, sn, a[j], b[j]);
           }
-          add(o[2 * c], a);
-          add(o[2 * c + 1], b);
-          __builtin_amdgcn_sched_barrier(0);
+          add(c, a, b);
         });
       }
     }
@@ -483,10 +572,15 @@ __device__ __forceinline__ void attend_fp4(const Fp4Params& f, const RopeParams&
   if (tiles > 0) fill(first, ring);
   if (tiles > 1) fill(first + kStepRows, ring + St::kBytes);
   // The query rows have arrived from here on.  Without this the wait for them would sit in the loop, and wait for tiles as well.
+  if constexpr (!kMx) {
 #pragma unroll
-  for (int part = 0; part < kQueryParts; ++part)
+    for (int part = 0; part < kQueryParts; ++part)
 #pragma unroll
-    for (int c = 0; c < NC; ++c) asm volatile("" : "+v"(qf[part][c]));
+      for (int c = 0; c < NC; ++c) asm volatile("" : "+v"(qf[part][c]));
+  } else {
+#pragma unroll
+    for (int part = 0; part < kQueryParts; ++part) asm volatile("" : "+v"(qx[part]), "+v"(q_unit[part]));
+  }
   int stage = 0;
   for (int i = 0; i < tiles; ++i) {
     const int base = first + i * kStepRows;
@@ -506,14 +600,17 @@ __device__ __forceinline__ void attend_fp4(const Fp4Params& f, const RopeParams&
   auto red = [&](int wv, int col, int j) VEC_INLINE { return reinterpret_cast<float*>(fp4_lds + wv * kWaveBytes) + col * kRedStride + j; };
   auto ml = [&](int wv, int what, int col) VEC_INLINE { return reinterpret_cast<float*>(fp4_lds + wv * kWaveBytes) + 16 * kRedStride + what * 16 + col; };
   wave_fence();
-  // lane (m, quarter): column m, dims of lane 4 quarter + i
+  // lane (m, quarter): column m, dims of lane 4 quarter + i; kPer of them, or of every other one, lie side by side
+  constexpr int kPer = kQuad ? (apart ? kDims / 4 : kDims / 2) : (apart ? kDims / 2 : kDims);
+  constexpr int kWide = kPer < 4 ? kPer : 4;
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int j = 0; j < NT; j += kDims / 2) {
-      const int dim = apart ? j / (kDims / 2) * (D / 2) + kDims / 2 * (4 * quarter + i) : kDims * (4 * quarter + i) + j;
-#pragma unroll
-      for (int e = 0; e < kDims / 2; e += 2) *reinterpret_cast<f32x2*>(red(wave, m, dim + e)) = f32x2{o[j + e][i], o[j + e + 1][i]};
+    for (int j = 0; j < NT; j += kWide) {
+      float* to = red(wave, m, j / kPer * (kQuad ? D / 4 : D / 2) + kPer * (4 * quarter + i) + j % kPer);
+      if constexpr (kWide == 4) *reinterpret_cast<f32x4*>(to) = f32x4{o[j][i], o[j + 1][i], o[j + 2][i], o[j + 3][i]};
+      else if constexpr (kWide == 2) *reinterpret_cast<f32x2*>(to) = f32x2{o[j][i], o[j + 1][i]};
+      else *to = o[j][i];
     }
   if (quarter == 0) {
     *ml(wave, 0, m) = ref;                             // minus infinity of a wave without rows: its share is 0 without a branch
@@ -531,11 +628,18 @@ __device__ __forceinline__ void attend_fp4(const Fp4Params& f, const RopeParams&
 #pragma unroll
     for (int wv = 0; wv < DW; ++wv) {
       const float sc = fast_exp2(*ml(wv, 0, g) - safe);
-      f32x4 x = *reinterpret_cast<const f32x4*>(red(wv, g, j));
-      if constexpr (SIDE) x += *reinterpret_cast<const f32x4*>(red(wv, 8 + g, j));
+      f32x4 x;
+      if constexpr (kQuad) {
+        const f32x2 even = *reinterpret_cast<const f32x2*>(red(wv, g, j / 2)) + *reinterpret_cast<const f32x2*>(red(wv, 4 + g, j / 2));
+        const f32x2 odd = *reinterpret_cast<const f32x2*>(red(wv, 8 + g, j / 2)) + *reinterpret_cast<const f32x2*>(red(wv, 12 + g, j / 2));
+        x = f32x4{even[0], odd[0], even[1], odd[1]};
+      } else {
+        x = *reinterpret_cast<const f32x4*>(red(wv, g, j));
+        if constexpr (kSide) x += *reinterpret_cast<const f32x4*>(red(wv, 8 + g, j));
+      }
 #pragma unroll
       for (int e = 0; e < 4; ++e) a[e] = fmaf(x[e], sc, a[e]);
-      l = fmaf(SIDE ? *ml(wv, 1, g) + *ml(wv, 1, 8 + g) : *ml(wv, 1, g), sc, l);
+      l = fmaf(COLS == 16 ? *ml(wv, 1, g) : *ml(wv, 1, g) + *ml(wv, 1, COLS + g), sc, l);
     }
     *reinterpret_cast<f32x4_u*>(out + 2 * G + i) = a;
     if (j == 0) {
@@ -545,37 +649,40 @@ __device__ __forceinline__ void attend_fp4(const Fp4Params& f, const RopeParams&
   }
 }
 
-template <typename T, int D, bool SIDE, Fp4RowKind APPROX>
+template <typename T, int D, int COLS, Fp4RowKind APPROX>
 __global__ __launch_bounds__(DT_, 3) void decode_split_fp4_kernel(Fp4Params f, RopeParams rp) {
   const SplitRows r = grid_split<DW * kFp4TileRows>(f.d);
-  if (r.is_apx) attend_fp4<T, D, SIDE, APPROX>(f, rp, r, (int)threadIdx.x);
-  else attend_fp4<T, D, SIDE, Fp4RowKind::kRetained>(f, rp, r, (int)threadIdx.x);
+  if (r.is_apx) attend_fp4<T, D, COLS, APPROX>(f, rp, r, (int)threadIdx.x);
+  else attend_fp4<T, D, COLS, Fp4RowKind::kRetained>(f, rp, r, (int)threadIdx.x);
 }
 
-template <typename T, int D, bool SIDE, Fp4RowKind APPROX>
+template <typename T, int D, int COLS, Fp4RowKind APPROX>
 int launch_split_fp4(const Fp4Params& f, const RopeParams* rope, hipStream_t stream) {
   const dim3 grid(f.d.splits_ret + f.d.splits_apx, f.d.Hkv, f.d.B);
   constexpr int lds = DW * kFp4Stages * Fp4Stage<D>::kBytes;
-  VEC_HIP(set_max_lds(reinterpret_cast<const void*>(decode_split_fp4_kernel<T, D, SIDE, APPROX>), lds));
-  VEC_LAUNCH(K_DECODE_SPLIT, (decode_split_fp4_kernel<T, D, SIDE, APPROX>), grid, dim3(DT_), lds, stream, f, rope ? *rope : RopeParams{});
+  constexpr auto kernel = decode_split_fp4_kernel<T, D, COLS, APPROX>;
+  VEC_HIP(set_max_lds(reinterpret_cast<const void*>(kernel), lds));
+  VEC_LAUNCH(K_DECODE_SPLIT, kernel, grid, dim3(DT_), lds, stream, f, rope ? *rope : RopeParams{});
   VEC_HIP(hipGetLastError());
   return VECTOR_OK;
 }
 
-template <typename T, int D, bool SIDE>
+template <typename T, int D, int COLS>
 int run_split_fp4(Fp4Params& f, const RopeParams* rope, hipStream_t stream) {
   pick_splits_fp4(f.d.B, f.d.Hkv, f.d.cap_retain, f.d.n_approx, f.d.splits_ret, f.d.splits_apx);
-  if (!rope || f.d.n_approx == 0) return launch_split_fp4<T, D, SIDE, Fp4RowKind::kApprox>(f, nullptr, stream);
-  return rope->interleaved ? launch_split_fp4<T, D, SIDE, Fp4RowKind::kTurnedNext>(f, rope, stream)
-                           : launch_split_fp4<T, D, SIDE, Fp4RowKind::kTurnedApart>(f, rope, stream);
+  if (!rope || f.d.n_approx == 0) return launch_split_fp4<T, D, COLS, Fp4RowKind::kApprox>(f, nullptr, stream);
+  return rope->interleaved ? launch_split_fp4<T, D, COLS, Fp4RowKind::kTurnedNext>(f, rope, stream)
+                           : launch_split_fp4<T, D, COLS, Fp4RowKind::kTurnedApart>(f, rope, stream);
 }
 
 template <typename T, int D>
 int run_fp4(Fp4Params& f, const RopeParams* rope, hipStream_t stream) {
   if constexpr (sizeof(T) == 2) {
-    if (f.d.Hq / f.d.Hkv <= 8) return run_split_fp4<T, D, true>(f, rope, stream);
+    const int G = f.d.Hq / f.d.Hkv;
+    if (G <= 4) return run_split_fp4<T, D, 4>(f, rope, stream);
+    if (G <= 8) return run_split_fp4<T, D, 8>(f, rope, stream);
   }
-  return run_split_fp4<T, D, false>(f, rope, stream);
+  return run_split_fp4<T, D, 16>(f, rope, stream);
 }
 
 }  // namespace

@@ -16,6 +16,8 @@ constexpr int fp4_scale_bytes(int head_dim) { return head_dim / kFp4Block; }
 
 typedef __attribute__((ext_vector_type(2))) float f32x2;
 typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+typedef __attribute__((ext_vector_type(8))) int i32x8;
+typedef __attribute__((ext_vector_type(2))) short s16x2;
 typedef __attribute__((ext_vector_type(4), aligned(4))) uint32_t u32x4_a4;   // scales of rows at any row
 typedef __attribute__((ext_vector_type(4), aligned(2))) uint32_t u32x4_a2;
 

@@ -398,3 +398,19 @@ def test_serving_from_prompts_to_steps():
                     p /= p.sum()
                     assert (np.abs(got[b, h * G + g] - p @ vv) <= 2.0 ** -14 * (p @ np.abs(vv)) + 1e-30).all(), f"step {s}"
     assert taken == H * sum(-(-(n + steps) // R) for n in lens) and live.tolist() == (lens + steps).tolist()
+
+
+@pytest.mark.parametrize("d,G,rope", [(128, 4, False), (128, 4, True), (64, 2, False), (64, 5, True), (128, 16, False), (128, 10, True)])
+@pytest.mark.parametrize("layout", ["blocks", "sequences", "paged16", "paged64"])
+def test_sequences_of_different_lengths(d, G, rope, layout):
+    """Enough rows by the capacities for the cuts that the device makes; the live lengths are anything."""
+    rng = np.random.default_rng(d + G)
+    lens = [int(x) for x in rng.integers(0, 700, 24)]
+    lens[3], lens[4], lens[11], lens[23] = 0, 1, 1500, 0
+    apx = [int(x) for x in rng.integers(0, 90, 24)]
+    apx[0], apx[4], apx[23] = 0, 200, 0
+    kw = dict(H=8, G=G, d=d, rope=rope, interleaved=G == 10, layout="paged" if layout.startswith("paged") else layout, room=100, block_rows=64 if layout == "paged64" else 16)
+    p = Problem(lens, apx if layout == "sequences" else 40, **kw)
+    if layout == "sequences":
+        p.cache.cap_retain, p.cache.n_approx = 1 << 20, max(apx)
+    p.check(True, layout)
