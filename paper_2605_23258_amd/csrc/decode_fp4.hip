@@ -134,73 +134,13 @@ __device__ __forceinline__ void attend_fp4(const Fp4Params& f, const RopeParams&
   u32x4 qf[kMx ? 1 : kQueryParts][kMx ? 1 : NC];
   i32x8 qx[kMx ? kQueryParts : 1];
   int q_unit[kMx ? kQueryParts : 1];
-  if constexpr (kMx) {
-    // A row in two fp8 parts under a scale for every 32 dims: four bits and the four behind them, all that bf16 has; an element far below its
-    // block's largest is off by 2^-22 of that at most.  The matrix core takes 16 dims from 16 quarter on and 16 from 64 + 16 quarter
-    // on from a lane, and the scale of dims 32 quarter .. (compared with one-hot operands); a block's dims are in two lanes.
-    float x[2][16];
-    int top[2];
+  u32x4 q_raw[sizeof(T) == 2 ? NC : 2 * NC];
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      load8(q_row + half * 64 + quarter * 16, x[half]);
-      load8(q_row + half * 64 + quarter * 16 + 8, x[half] + 8);
-      uint32_t most = max(top_bits8(x[half]), top_bits8(x[half] + 8));
-      most = max(most, (uint32_t)__shfl_xor((int)most, 16, kWave));
-      // the largest between 128 and 256 units; an infinite or NaN element: NaN, in the whole block
-      top[half] = most >= 0x7f800000u ? 255 : min(max((int)(most >> 23) - 7, 6), 254);
-    }
-    const int first = __shfl(top[0], m + (quarter & 1) * 32, kWave), second = __shfl(top[1], m + (quarter & 1) * 32, kWave);
-    const int own = quarter < 2 ? first : second;      // of block `quarter`
-#pragma unroll
-    for (int part = 0; part < kQueryParts; ++part) q_unit[part] = own == 255 ? 255 : own - (lo || part == 1 ? 5 : 0);
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      const int byte = top[half] == 255 ? 127 : top[half];
-      const float unit = fp4_unit((uint32_t)byte), small = fp4_unit((uint32_t)(byte - 5));
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        s16x2 hi = {0, 0}, rest = {0, 0};
-        float y[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] = __uint_as_float(__float_as_uint(x[half][4 * w + e]) ^ f.flip);
-        hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(hi, y[0], y[1], unit, false);
-        hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(hi, y[2], y[3], unit, true);
-        const int word = __builtin_bit_cast(int, hi);
-        const f32x2 back0 = __builtin_bit_cast(f32x2, __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(word, unit, false));
-        const f32x2 back1 = __builtin_bit_cast(f32x2, __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(word, unit, true));
-        rest = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(rest, y[0] - back0[0], y[1] - back0[1], small, false);
-        rest = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(rest, y[2] - back1[0], y[3] - back1[1], small, true);
-        if constexpr (kQueryParts == 2) {
-          qx[0][half * 4 + w] = word;
-          qx[1][half * 4 + w] = __builtin_bit_cast(int, rest);
-        } else {
-          qx[0][half * 4 + w] = lo ? __builtin_bit_cast(int, rest) : word;
-        }
-      }
-    }
-  } else {
-#pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      const T* q = q_row + quarter * (D / 4) + c * 8;
-      if constexpr (!kExact) {
-        qf[0][c] = *reinterpret_cast<const u32x4*>(q) ^ (f.flip | f.flip >> 16);
-      } else {
-        float x[8];
-        load8(q, x);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(__float_as_uint(x[e]) ^ f.flip);
-#pragma unroll
-        for (int part = 0; part < kQueryParts; ++part) {
-          float y[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) { y[e] = leading(x[e]); x[e] -= y[e]; }
-#pragma unroll
-          for (int e = 0; e < 4; ++e) qf[part][c][e] = high_halves(y[2 * e], y[2 * e + 1]);
-        }
-      }
-    }
+  for (int c = 0; c < NC; ++c) {
+    const int at = kMx ? c / 2 * 64 + quarter * 16 + c % 2 * 8 : quarter * (D / 4) + c * 8;
+    q_raw[c] = *reinterpret_cast<const u32x4*>(q_row + at);
+    if constexpr (kExact) q_raw[NC + c] = *reinterpret_cast<const u32x4*>(q_row + at + 4);
   }
-
   // The sum of a column's weights is one more row of the second product, of ones: the same in every lane, and of the weights as they
   // went in.
   f32x4 o[NT], o_sum = zero;
@@ -571,6 +511,71 @@ __device__ __forceinline__ void attend_fp4(const Fp4Params& f, const RopeParams&
   const int first = row_begin + wave * kFp4TileRows;
   if (tiles > 0) fill(first, ring);
   if (tiles > 1) fill(first + kStepRows, ring + St::kBytes);
+  // the query rows in operand order; the first tiles are on their way
+  if constexpr (kMx) {
+    // A row in two fp8 parts under a scale for every 32 dims: four bits and the four behind them, all that bf16 has; an element far below its
+    // block's largest is off by 2^-22 of that at most.  The matrix core takes 16 dims from 16 quarter on and 16 from 64 + 16 quarter
+    // on from a lane, and the scale of dims 32 quarter .. (compared with one-hot operands); a block's dims are in two lanes.
+    float x[2][16];
+    int top[2];
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x[half][e] = (e & 1) ? bf16_hi(q_raw[2 * half + e / 8][e % 8 / 2]) : bf16_lo(q_raw[2 * half + e / 8][e % 8 / 2]);
+      uint32_t most = max(top_bits8(x[half]), top_bits8(x[half] + 8));
+      most = max(most, (uint32_t)__shfl_xor((int)most, 16, kWave));
+      // the largest between 128 and 256 units; an infinite or NaN element: NaN, in the whole block
+      top[half] = most >= 0x7f800000u ? 255 : min(max((int)(most >> 23) - 7, 6), 254);
+    }
+    const int first = __shfl(top[0], m + (quarter & 1) * 32, kWave), second = __shfl(top[1], m + (quarter & 1) * 32, kWave);
+    const int own = quarter < 2 ? first : second;      // of block `quarter`
+#pragma unroll
+    for (int part = 0; part < kQueryParts; ++part) q_unit[part] = own == 255 ? 255 : own - (lo || part == 1 ? 5 : 0);
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const int byte = top[half] == 255 ? 127 : top[half];
+      const float unit = fp4_unit((uint32_t)byte), small = fp4_unit((uint32_t)(byte - 5));
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        s16x2 hi = {0, 0}, rest = {0, 0};
+        float y[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = __uint_as_float(__float_as_uint(x[half][4 * w + e]) ^ f.flip);
+        hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(hi, y[0], y[1], unit, false);
+        hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(hi, y[2], y[3], unit, true);
+        const int word = __builtin_bit_cast(int, hi);
+        const f32x2 back0 = __builtin_bit_cast(f32x2, __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(word, unit, false));
+        const f32x2 back1 = __builtin_bit_cast(f32x2, __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(word, unit, true));
+        rest = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(rest, y[0] - back0[0], y[1] - back0[1], small, false);
+        rest = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(rest, y[2] - back1[0], y[3] - back1[1], small, true);
+        if constexpr (kQueryParts == 2) {
+          qx[0][half * 4 + w] = word;
+          qx[1][half * 4 + w] = __builtin_bit_cast(int, rest);
+        } else {
+          qx[0][half * 4 + w] = lo ? __builtin_bit_cast(int, rest) : word;
+        }
+      }
+    }
+  } else {
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      if constexpr (!kExact) {
+        qf[0][c] = q_raw[c] ^ (f.flip | f.flip >> 16);
+      } else {
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(q_raw[c + (e >= 4 ? NC : 0)][e % 4] ^ f.flip);
+#pragma unroll
+        for (int part = 0; part < kQueryParts; ++part) {
+          float y[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) { y[e] = leading(x[e]); x[e] -= y[e]; }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) qf[part][c][e] = high_halves(y[2 * e], y[2 * e + 1]);
+        }
+      }
+    }
+  }
   // The query rows have arrived from here on.  Without this the wait for them would sit in the loop, and wait for tiles as well.
   if constexpr (!kMx) {
 #pragma unroll
@@ -669,7 +674,7 @@ int launch_split_fp4(const Fp4Params& f, const RopeParams* rope, hipStream_t str
 
 template <typename T, int D, int COLS>
 int run_split_fp4(Fp4Params& f, const RopeParams* rope, hipStream_t stream) {
-  pick_splits_fp4(f.d.B, f.d.Hkv, f.d.cap_retain, f.d.n_approx, f.d.splits_ret, f.d.splits_apx);
+  pick_splits_fp4(f.d.B, f.d.Hkv, f.d.cap_retain, f.d.n_approx, rope ? kFp4Turned : kFp4Approx, f.d.splits_ret, f.d.splits_apx);
   if (!rope || f.d.n_approx == 0) return launch_split_fp4<T, D, COLS, Fp4RowKind::kApprox>(f, nullptr, stream);
   return rope->interleaved ? launch_split_fp4<T, D, COLS, Fp4RowKind::kTurnedNext>(f, rope, stream)
                            : launch_split_fp4<T, D, COLS, Fp4RowKind::kTurnedApart>(f, rope, stream);

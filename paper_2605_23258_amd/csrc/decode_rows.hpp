@@ -164,17 +164,37 @@ inline bool pick_one_round(const SplitCosts& c, int batch, int n_kv_heads, int c
   return best >= 0.0;
 }
 
-// Caches held in 4 bits: as many workgroups as run at the same time, pieces of equal length in steps of 128 rows.
+// Caches held in 4 bits: as many workgroups as run at the same time, cut so that the longest piece is the shortest; steps of 128 rows.
+// What a step of approximated rows takes, in steps of retained ones: they have half the bytes, but as much arithmetic, and sines and cosines
+// where they are turned back.  Split launch, us, equal pieces / these: 24 unequal sequences of up to 16000 tokens on rotated keys 26.3 / 22.0;
+// 16 of 32768 33.4 / 33.1, on plain keys 21.6 / 21.4, four 11.7 / 11.3.  More workgroups than run at the same time (1024, 1536, 2304) are slower: 16 of
+// 32768 23.8 / 26.7 / 26.7 / 27.2, 24 unequal ones 16.9 / 18.4 / 20.0 / 19.5; the plan of unequal bf16 caches (PlannedSplits), too, since a CU that has
+// done its short pieces leaves the memory to the others: 24 unequal ones 17.4 / 18.2, 48 of up to 4000 19.2 / 23.0.
 constexpr int kFp4StepRows = 128, kFp4PerCu = 3;
-inline void pick_splits_fp4(int batch, int n_kv_heads, int cap_retain, int n_approx, int& s_ret, int& s_apx) {
+constexpr double kFp4Approx = 0.8, kFp4Turned = 2.5;
+inline void pick_splits_fp4(int batch, int n_kv_heads, int cap_retain, int n_approx, double apx_cost, int& s_ret, int& s_apx) {
   const int64_t steps_r = ((int64_t)cap_retain + kFp4StepRows - 1) / kFp4StepRows, steps_a = ((int64_t)n_approx + kFp4StepRows - 1) / kFp4StepRows;
   const int64_t pairs = (int64_t)batch * n_kv_heads, at_once = 256 * kFp4PerCu;
-  const int64_t most = std::max<int64_t>(2, std::min<int64_t>(kMaxSplits, at_once / pairs));
-  int64_t piece = std::max<int64_t>(1, (steps_r + steps_a + most - 1) / most);
-  while ((steps_r + piece - 1) / piece + (steps_a + piece - 1) / piece > most && piece < steps_r + steps_a) ++piece;
-  s_ret = (int)((steps_r + piece - 1) / piece);
-  s_apx = (int)((steps_a + piece - 1) / piece);
-  if (s_ret + s_apx == 0) s_ret = 1;             // nothing cached: one workgroup writes the empty partial
+  const int most = (int)std::max<int64_t>(2, std::min<int64_t>(kMaxSplits, at_once / pairs));
+  s_ret = steps_r > 0 || steps_a == 0 ? 1 : 0;   // nothing cached: one workgroup writes the empty partial
+  s_apx = steps_a > 0 ? 1 : 0;
+  if (steps_r == 0 || steps_a == 0) {
+    const int64_t steps = steps_r + steps_a, longest = std::max<int64_t>(1, (steps + most - 1) / most);
+    (steps_a > 0 ? s_apx : s_ret) = (int)std::max<int64_t>(1, (steps + longest - 1) / longest);
+    return;
+  }
+  double best = -1.0;
+  for (int r = 1; r < most && r <= steps_r; ++r) {
+    const int64_t long_r = (steps_r + r - 1) / r, a = std::min<int64_t>(most - r, steps_a), long_a = (steps_a + a - 1) / a;
+    const double t = std::max((double)long_r, apx_cost * (double)long_a);
+    if (best < 0.0 || t < best) {
+      best = t;
+      s_ret = (int)((steps_r + long_r - 1) / long_r);
+      // no more pieces of approximated rows than bring them down to that
+      const int64_t enough = std::max<int64_t>(long_a, (int64_t)(t / apx_cost));
+      s_apx = (int)((steps_a + enough - 1) / enough);
+    }
+  }
 }
 
 // Sequences of different lengths, whose live rows only the device knows, cut by a plan that the split launch makes (PlannedSplits in
