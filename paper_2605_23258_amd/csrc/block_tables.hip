@@ -3,7 +3,8 @@
 // Which blocks a request gets follows from the requests before it: one running sum over the batch of the blocks they need
 // and one of their tokens.  There is one launch, without workspace: every workgroup makes both sums for itself (a batch of up to kMaxRequests lengths,
 // which lie in the L2 after the first workgroup's read) and then writes its part of the slots or of the table.  A second launch that
-// only read the sums would cost more than they do.  What is left is bound by the writes: 8 bytes per token and KV head.
+// only read the sums would cost more than they do.  Small batches are a chain of two trips to memory (lengths; block ids); large ones are
+// bound by the writes, 8 bytes per token and KV head: two tokens a thread, 16 bytes a store.
 #include "common.hpp"
 #include "launch.hpp"
 
@@ -12,7 +13,8 @@ namespace vec {
 namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / kWave;
-constexpr int kTokensPerGroup = 1024;        // slots a workgroup writes for every KV head
+constexpr int kTokensPerGroup = 512;         // slots a workgroup writes for every KV head
+constexpr int kHeadsAtOnce = 4;
 constexpr int kPairsPerGroup = 8;            // (request, KV head) rows of the table a workgroup writes
 
 struct TableParams {
@@ -41,67 +43,110 @@ __device__ __forceinline__ bool admitted(const TableParams& p, const Request& r,
   return (wanted(p, r) == 0 || blocks <= p.n_free) && (!p.slots || r.len == r.held || tokens <= p.n_slots);
 }
 
-__device__ __forceinline__ int64_t wave_incl_scan64(int64_t x, int lane) {
-#pragma unroll
-  for (int o = 1; o < kWave; o <<= 1) {
-    const int64_t y = __shfl_up(x, o, kWave);
-    if (lane >= o) x += y;
-  }
-  return x;
+// running sum over the lanes that stops at 2^32 - 1 (of numbers below 2^31)
+template <int CTRL, int ROW_MASK> __device__ __forceinline__ uint32_t add_upto(uint32_t v) {
+  return __builtin_elementwise_add_sat(v, (uint32_t)dpp_take<CTRL, ROW_MASK>((int)v));
+}
+__device__ __forceinline__ uint32_t wave_incl_scan_upto(uint32_t v) {
+  v = add_upto<0x111, 0xf>(v);
+  v = add_upto<0x112, 0xf>(v);
+  v = add_upto<0x114, 0xf>(v);
+  v = add_upto<0x118, 0xf>(v);
+  v = add_upto<0x142, 0xa>(v);
+  return add_upto<0x143, 0xc>(v);
 }
 
 __global__ __launch_bounds__(kThreads) void block_tables_kernel(TableParams p) {
-  extern __shared__ int sums[];              // [B + 1] blocks of one KV head up to a request times KV heads, [B + 1] tokens
-  __shared__ int64_t wave_blocks[kWaves], wave_tokens[kWaves];
-  int *blocks = sums, *tokens = sums + p.B + 1;
+  // of request b - 1: blocks up to it, of all KV heads; tokens up to it; and its lengths
+  extern __shared__ __align__(16) int lds[];
+  __shared__ int wave_blocks[kWaves];
+  __shared__ uint32_t wave_tokens[kWaves];
+  int *blocks = lds, *tokens = lds + p.B + 1;
+  Request* requests = reinterpret_cast<Request*>(lds + 2 * (p.B + 1));
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  int64_t base_blocks = 0, base_tokens = 0;
+  int base_blocks = 0;                       // at most B * H * per_seq, which the host has checked
+  uint32_t base_tokens = 0;
   if (tid == 0) blocks[0] = tokens[0] = 0;
   for (int b0 = 0; b0 < p.B; b0 += kThreads) {
     const int b = b0 + tid;
     const Request r = b < p.B ? request(p, b) : Request{0, 0};
-    int64_t nb = wave_incl_scan64((int64_t)wanted(p, r) * p.H, lane), nt = wave_incl_scan64((int64_t)r.len - r.held, lane);
+    int nb = wave_incl_scan_dpp(wanted(p, r) * p.H);
+    uint32_t nt = wave_incl_scan_upto((uint32_t)(r.len - r.held));
+    if (b0 > 0) __syncthreads();             // the waves' sums of the round before have been read
     if (lane == 63) { wave_blocks[wave] = nb; wave_tokens[wave] = nt; }
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
-      if (w < wave) { nb += wave_blocks[w]; nt += wave_tokens[w]; }
+      if (w < wave) { nb += wave_blocks[w]; nt = __builtin_elementwise_add_sat(nt, wave_tokens[w]); }
     }
     nb += base_blocks;
-    nt += base_tokens;
+    nt = __builtin_elementwise_add_sat(nt, base_tokens);
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) { base_blocks += wave_blocks[w]; base_tokens += wave_tokens[w]; }
-    if (b < p.B) {
-      blocks[b + 1] = (int)nb;                                  // at most B * H * per_seq, which the host has checked
-      tokens[b + 1] = (int)min(nt, (int64_t)INT32_MAX);         // slots end before that
+    for (int w = 0; w < kWaves; ++w) {
+      base_blocks += wave_blocks[w];
+      base_tokens = __builtin_elementwise_add_sat(base_tokens, wave_tokens[w]);
     }
-    __syncthreads();
+    if (b < p.B) {
+      blocks[b + 1] = nb;
+      tokens[b + 1] = (int)min(nt, (uint32_t)INT32_MAX);        // slots end before that
+      requests[b] = r;
+    }
   }
+  __syncthreads();
 
   if ((int)blockIdx.x < p.slot_groups) {
-    // slots: a thread takes a token for all KV heads; neighbours are tokens of one request, mostly
+    // slots: a thread takes two tokens for all KV heads; neighbours are tokens of one request, mostly
     const int t0 = blockIdx.x * kTokensPerGroup;
-    for (int t = t0 + tid; t < min(t0 + kTokensPerGroup, p.n_slots); t += kThreads) {
+    for (int t = t0 + 2 * tid; t < min(t0 + kTokensPerGroup, p.n_slots); t += 2 * kThreads) {
       // the request b with tokens[b] <= t < tokens[b + 1]
       int lo = 0, hi = p.B;                  // tokens[lo] <= t; hi == B or t < tokens[hi]
       while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
         if (tokens[mid] <= t) lo = mid; else hi = mid;
       }
-      const int b = lo;
-      const bool any = t < tokens[b + 1];    // behind the last token: no slot
-      const Request r = request(p, b);
-      const bool ok = any && admitted(p, r, blocks[b + 1], tokens[b + 1]);
-      const int pos = r.held + (t - tokens[b]), before = blocks_of(r.held, p.shift), n = wanted(p, r), at = pos >> p.shift;
-      for (int h = 0; h < p.H; ++h) {
-        int64_t slot = -1;
-        if (ok) {
-          // a new block comes from the free list, a block that the request holds from the table (this launch does not write these)
-          const int id = at >= before ? (p.free_blocks ? p.free_blocks[blocks[b] + h * n + at - before] : blocks[b] + h * n + at - before)
-                                      : p.table[((int64_t)b * p.H + h) * p.per_seq + at];
-          slot = ((int64_t)id << p.shift) + (pos & ((1 << p.shift) - 1));
+      // where a token's block id lies: in the free list, or (a block that the request holds, which this launch does not write) in the
+      // table, and how far the next KV head's lies behind it
+      const int32_t* at[2];
+      int step[2], row[2], id[2];
+      bool ok[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        if (i == 1) {
+          while (lo + 1 < p.B && tokens[lo + 1] <= t + 1) ++lo;
         }
-        p.slots[(int64_t)h * p.n_slots + t] = slot;
+        const Request r = requests[lo];
+        ok[i] = t + i < tokens[lo + 1] && admitted(p, r, blocks[lo + 1], tokens[lo + 1]);      // behind the last token there are none
+        const int pos = r.held + (t + i - tokens[lo]), before = blocks_of(r.held, p.shift), n = wanted(p, r), block = pos >> p.shift;
+        row[i] = pos & ((1 << p.shift) - 1);
+        const bool fresh = block >= before;
+        id[i] = blocks[lo] + block - before;
+        step[i] = fresh ? n : p.per_seq;
+        at[i] = fresh ? (p.free_blocks ? p.free_blocks + id[i] : nullptr) : p.table + (int64_t)lo * p.H * p.per_seq + block;
+      }
+      int64_t* to = p.slots + t;
+      const bool both = t + 1 < p.n_slots;
+      for (int h0 = 0; h0 < p.H; h0 += kHeadsAtOnce) {
+        int64_t slot[kHeadsAtOnce][2];
+#pragma unroll
+        for (int u = 0; u < kHeadsAtOnce; ++u)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const int h = min(h0 + u, p.H - 1);
+            int block = id[i] + h * step[i];
+            if (ok[i] && at[i]) block = at[i][(int64_t)h * step[i]];
+            slot[u][i] = ok[i] ? ((int64_t)block << p.shift) + row[i] : -1;
+          }
+#pragma unroll
+        for (int u = 0; u < kHeadsAtOnce; ++u) {
+          if (h0 + u >= p.H) break;
+          int64_t* out = to + (int64_t)(h0 + u) * p.n_slots;
+          if (both) {
+            typedef __attribute__((ext_vector_type(2), aligned(8))) int64_t i64x2;
+            *reinterpret_cast<i64x2*>(out) = i64x2{slot[u][0], slot[u][1]};
+          } else {
+            *out = slot[u][0];
+          }
+        }
       }
     }
     return;
@@ -109,7 +154,7 @@ __global__ __launch_bounds__(kThreads) void block_tables_kernel(TableParams p) {
   const int group = blockIdx.x - p.slot_groups;
   if (group == 0) {
     for (int b = tid; b < p.B; b += kThreads) {
-      const Request r = request(p, b);
+      const Request r = requests[b];
       p.live[b] = admitted(p, r, blocks[b + 1], tokens[b + 1]) ? r.len : r.held;
     }
   }
@@ -117,7 +162,7 @@ __global__ __launch_bounds__(kThreads) void block_tables_kernel(TableParams p) {
     // blocks taken: those of the admitted requests, which are the first ones that ask for any
     int taken = 0;
     for (int b = lane; b < p.B; b += kWave) {
-      const Request r = request(p, b);
+      const Request r = requests[b];
       if (wanted(p, r) > 0 && admitted(p, r, blocks[b + 1], tokens[b + 1])) taken = max(taken, blocks[b + 1]);
     }
 #pragma unroll
@@ -131,7 +176,7 @@ __global__ __launch_bounds__(kThreads) void block_tables_kernel(TableParams p) {
   const int pairs = p.B * p.H;
   for (int pair = group * kPairsPerGroup + wave; pair < min((group + 1) * kPairsPerGroup, pairs); pair += kWaves) {
     const int b = pair / p.H, h = pair % p.H;
-    const Request r = request(p, b);
+    const Request r = requests[b];
     const bool ok = admitted(p, r, blocks[b + 1], tokens[b + 1]);
     const int before = blocks_of(r.held, p.shift), n = ok ? wanted(p, r) : 0, first = blocks[b] + h * n;
     int32_t* row = p.table + (int64_t)pair * p.per_seq;
@@ -154,7 +199,9 @@ int launch_block_tables(const vector_blocks& v, int32_t* table, int32_t* live, i
   while ((1 << p.shift) < v.block_rows) ++p.shift;
   p.slot_groups = (p.n_slots + kTokensPerGroup - 1) / kTokensPerGroup;
   const int table_groups = (p.B * p.H + kPairsPerGroup - 1) / kPairsPerGroup;
-  VEC_LAUNCH(K_BLOCK_TABLES, block_tables_kernel, dim3(p.slot_groups + table_groups), dim3(kThreads), 2 * (p.B + 1) * sizeof(int), stream, p);
+  const size_t lds = 2 * (p.B + 1) * sizeof(int) + p.B * sizeof(Request);
+  VEC_HIP(set_max_lds(reinterpret_cast<const void*>(block_tables_kernel), lds));
+  VEC_LAUNCH(K_BLOCK_TABLES, block_tables_kernel, dim3(p.slot_groups + table_groups), dim3(kThreads), lds, stream, p);
   VEC_HIP(hipGetLastError());
   return VECTOR_OK;
 }

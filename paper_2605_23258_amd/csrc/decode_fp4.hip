@@ -7,7 +7,8 @@
 // An element in 4 bits times its scale has two significant bits and is a bf16 number exactly; the weights go in as parts of eight bits each.
 //
 // A wave takes 32 rows at a time and waits for no other before the end.  Their codes and scales go from memory straight into a ring of its
-// own in LDS (Fp4Stage), so that what is on its way takes no registers, and are read back in the matrix cores' order:
+// own in LDS (Fp4Stage), past the caches (16 whole caches of 32768 tokens 105 us with them, 91 without: 6.2 TB/s), so that what is on its way
+// takes no registers, and are read back in the matrix cores' order:
 //   scores   S[t][g] = sum_e K[t][e] q[g][e]      A = K: lane (m, quarter) holds D / 4 consecutive elements of a row, which is one read and
 //                                                  one scale.  128 dims: as they are, in 4 bits with their scales, against query rows in
 //                                                  two fp8 parts (kMx); 64 dims and fp32: converted to bf16
@@ -193,7 +194,7 @@ __device__ __forceinline__ void attend_fp4(const Fp4Params& f, const RopeParams&
     if (base + kFp4TileRows <= stored && lo && hi) {   // uniform: rows that are all there
       auto codes = [&](const uint8_t* from, int64_t at, uint32_t dst) VEC_INLINE {
 #pragma unroll
-        for (int i = 0; i < St::kLoads; ++i) load_to_lds16(dst + i * 1024, from + (at + i * (8 / St::kLoads)) * kCode, in_code);
+        for (int i = 0; i < St::kLoads; ++i) load_to_lds16_once(dst + i * 1024, from + (at + i * (8 / St::kLoads)) * kCode, in_code);
       };
       const void* s = in_scale + (small_blocks && scale_row >= 16 ? at_hi : at_lo) * kScale;
       if (!small_blocks || is_apx) {
