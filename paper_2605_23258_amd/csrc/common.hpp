@@ -324,7 +324,8 @@ __device__ __forceinline__ void load_to_lds16(uint32_t lds, const void* g) {
 __device__ __forceinline__ void load_to_lds16_once(uint32_t lds, const void* g, uint32_t offset) {
   const uint64_t at = (uint64_t)g;
   const uint64_t same = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(at >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)at);
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(__builtin_amdgcn_readfirstlane((int)lds)), "v"(offset), "s"(same) : "m0", "memory");
+  // (five wait states, should the address's scalar registers have come from the vector unit just before)
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(__builtin_amdgcn_readfirstlane((int)lds)), "v"(offset), "s"(same) : "m0", "memory");
 }
 __device__ __forceinline__ void load_to_lds4(uint32_t lds, const void* g) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(__builtin_amdgcn_readfirstlane((int)lds)), "v"(g) : "m0", "memory");

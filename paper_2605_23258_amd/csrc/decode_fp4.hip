@@ -587,6 +587,10 @@ __device__ __forceinline__ void attend_fp4(const Fp4Params& f, const RopeParams&
 #pragma unroll
     for (int part = 0; part < kQueryParts; ++part) asm volatile("" : "+v"(qx[part]), "+v"(q_unit[part]));
   }
+  if constexpr (turned) {
+#pragma unroll
+    for (int e = 0; e < kDims / 2; ++e) asm volatile("" : "+v"(t_hi[e]), "+v"(t_lo[e]));
+  }
   int stage = 0;
   for (int i = 0; i < tiles; ++i) {
     const int base = first + i * kStepRows;
