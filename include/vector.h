@@ -399,7 +399,7 @@ VECTOR_API int vector_decode_step_rope(const vector_cache* cache, const vector_r
  * vector_cache and vector_cache_fp4) needs for the next tokens of a batch, without the lengths coming to the host.
  * Request b holds blocks for len_held[b] rows per KV head and asks for len[b]; with R = block_rows it needs
  * n_b = ceil(len[b] / R) - ceil(len_held[b] / R) more blocks per KV head.  Requests are admitted in order while the free
- * blocks last: b is admitted if n_b = 0, or if n_kv_heads * (n_0 + .. + n_b) <= n_free; and, where slots are asked for
+ * blocks last: b is admitted if n_b = 0, or if n_kv_heads * (n_0 + .. + n_b) blocks are left; and, where slots are asked for
  * and it has new tokens, if they all fit the slot map; never if len[b] is more than a row of the table has blocks for
  * (it then counts as needing none).  A length below zero counts as zero, len[b] below len_held[b] as len_held[b].
  *   block_table  device [batch, n_kv_heads, blocks_per_seq]: an admitted request's new blocks, KV head after KV head, are the next
@@ -410,9 +410,9 @@ VECTOR_API int vector_decode_step_rope(const vector_cache* cache, const vector_r
  *   slots        NULL (or n_slots 0): none are asked for; or device [n_kv_heads, n_slots]: the rows of the pools (block id * R + row in the block) of the
  *                new tokens, request after request (tokens len_held[b] .. len[b] - 1); -1 for tokens of requests that are not
  *                admitted and for columns behind the last token.  0 <= n_slots < 2^31 - 1.
- *   counts       device [VECTOR_BLOCK_COUNTS]: blocks taken from the front of free_blocks, blocks that all requests together need,
- *                new tokens of all requests (both stop at 2^31 - 1)
- * VECTOR_ERR_SHAPE: more than 4096 requests, or a table of 2^31 entries or more. */
+ *   counts       device [VECTOR_BLOCK_COUNTS]: blocks that this call takes from the front of free_blocks, blocks that all requests together
+ *                need, new tokens of all requests (at most 2^31 - 1).  Not the memory of n_used.
+ * VECTOR_ERR_SHAPE: more than 4096 requests, more than 2^26 (request, KV head) pairs, or a table of 2^31 entries or more. */
 typedef struct {
   int32_t batch, n_kv_heads;
   int32_t block_rows;            /* R: a power of two, at least 16                           */
@@ -422,6 +422,8 @@ typedef struct {
   const int32_t* len_held;       /* device [batch], or NULL: no request holds blocks yet     */
   const int32_t* len;            /* device [batch]                                           */
   const int32_t* free_blocks;    /* device [n_free]: ids of free blocks; NULL: 0, 1, 2, ..   */
+  const int32_t* n_used;         /* device [1], or NULL: as many of them, from the front, have been taken by calls before (0); add
+                                    counts[0] to it on the GPU, and no length or count ever has to come to the host */
 } vector_blocks;
 #define VECTOR_BLOCK_COUNTS 3
 VECTOR_API int vector_block_tables(const vector_blocks* blocks, int32_t* block_table, int32_t* len_live, int64_t* slots,
@@ -451,12 +453,13 @@ VECTOR_API int vector_compact_fp4(const vector_shape* shape, const void* k, cons
 /* Rows into pools of rows in 4 bits by slots (those of vector_block_tables, or any others): row t of KV head h of k (and of v,
  * which may be NULL with its pool) goes to row slots[h * seq_len + t] of the pools, which have pool_rows rows.  A row whose slot is
  * negative or not below pool_rows goes nowhere.  Slots must differ.  k, v: [Hkv, seq_len, d] with the shape's strides and dtype;
- * slots: device [Hkv, seq_len].  seq_len is not limited here. */
+ * slots: device [Hkv, seq_len].  seq_len may be up to 2^29 - 1 here (VECTOR_ERR_SHAPE beyond). */
 VECTOR_API int vector_store_fp4(const vector_shape* shape, const void* k, const void* v, const int64_t* slots, int64_t pool_rows,
                      uint8_t* k_pool, uint8_t* k_pool_scale, uint8_t* v_pool, uint8_t* v_pool_scale, void* stream);
 
 /* The values of rows in 4 bits: out[r] (device [n_rows, head_dim] of dtype) is row slots[r] of an array of pool_rows rows, row r where
- * slots is NULL; zeros where there is no such row.  The values of fp32 are exact; those of bf16 too. */
+ * slots is NULL; zeros where there is no such row.  The values are exact in either type.  VECTOR_ERR_SHAPE for 2^30 rows
+ * or more. */
 VECTOR_API int vector_load_fp4(int64_t n_rows, int32_t head_dim, int32_t dtype, const uint8_t* codes, const uint8_t* scales,
                     int64_t pool_rows, const int64_t* slots, void* out, void* stream);
 

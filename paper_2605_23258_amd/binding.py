@@ -105,14 +105,15 @@ def make_batch(seq_len, n_pool, n_approx, cap_retain):
 class Blocks(C.Structure):
     """vector_blocks: requests that ask for blocks of a paged cache."""
     _fields_ = [("batch", C.c_int32), ("n_kv_heads", C.c_int32), ("block_rows", C.c_int32), ("blocks_per_seq", C.c_int32),
-                ("n_free", C.c_int32), ("reserved", C.c_int32), ("len_held", C.c_void_p), ("len", C.c_void_p), ("free_blocks", C.c_void_p)]
+                ("n_free", C.c_int32), ("reserved", C.c_int32), ("len_held", C.c_void_p), ("len", C.c_void_p), ("free_blocks", C.c_void_p),
+                ("n_used", C.c_void_p)]
 
 
-def make_blocks(length, n_kv_heads: int, block_rows: int, blocks_per_seq: int, free, held=None) -> Blocks:
-    """Blocks from device int32 tensors: lengths asked for, ids of free blocks, and the lengths that the requests hold blocks for (None:
-    all requests are new).  The tensors have to outlive it."""
+def make_blocks(length, n_kv_heads: int, block_rows: int, blocks_per_seq: int, free, held=None, used=None) -> Blocks:
+    """Blocks from device int32 tensors: lengths asked for, ids of free blocks, the lengths that the requests hold blocks for (None:
+    all requests are new), and how many of the ids have been taken from the front (None: none).  The tensors have to outlive it."""
     return Blocks(batch=length.numel(), n_kv_heads=n_kv_heads, block_rows=block_rows, blocks_per_seq=blocks_per_seq, n_free=free.numel(),
-                  len_held=_ptr(held), len=_ptr(length), free_blocks=_ptr(free))
+                  len_held=_ptr(held), len=_ptr(length), free_blocks=_ptr(free), n_used=_ptr(used))
 
 
 class CacheFp4(C.Structure):

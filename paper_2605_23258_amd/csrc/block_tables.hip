@@ -18,7 +18,7 @@ constexpr int kHeadsAtOnce = 4;
 constexpr int kPairsPerGroup = 8;            // (request, KV head) rows of the table a workgroup writes
 
 struct TableParams {
-  const int32_t *held, *len, *free_blocks;
+  const int32_t *held, *len, *free_blocks, *used;
   int32_t *table, *live, *counts;
   int64_t* slots;
   int B, H, shift, per_seq, n_free, n_slots;
@@ -64,6 +64,10 @@ __global__ __launch_bounds__(kThreads) void block_tables_kernel(TableParams p) {
   int *blocks = lds, *tokens = lds + p.B + 1;
   Request* requests = reinterpret_cast<Request*>(lds + 2 * (p.B + 1));
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  // the list without what calls before have taken from its front; without a list, the first of the ids
+  const int first_id = p.used ? min(max(*p.used, 0), p.n_free) : 0;
+  p.n_free -= first_id;
+  if (p.free_blocks) p.free_blocks += first_id;
   int base_blocks = 0;                       // at most B * H * per_seq, which the host has checked
   uint32_t base_tokens = 0;
   if (tid == 0) blocks[0] = tokens[0] = 0;
@@ -132,7 +136,7 @@ __global__ __launch_bounds__(kThreads) void block_tables_kernel(TableParams p) {
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
             const int h = min(h0 + u, p.H - 1);
-            int block = id[i] + h * step[i];
+            int block = first_id + id[i] + h * step[i];
             if (ok[i] && at[i]) block = at[i][(int64_t)h * step[i]];
             slot[u][i] = ok[i] ? ((int64_t)block << p.shift) + row[i] : -1;
           }
@@ -183,7 +187,7 @@ __global__ __launch_bounds__(kThreads) void block_tables_kernel(TableParams p) {
     const int from = p.held ? before : 0, to = p.held ? before + n : p.per_seq;      // a new table is written whole
     for (int c = from + lane; c < to; c += kWave) {
       int id = 0;
-      if (c - before < n) id = p.free_blocks ? p.free_blocks[first + c - before] : first + c - before;
+      if (c - before < n) id = p.free_blocks ? p.free_blocks[first + c - before] : first_id + first + c - before;
       row[c] = id;
     }
   }
@@ -193,7 +197,7 @@ __global__ __launch_bounds__(kThreads) void block_tables_kernel(TableParams p) {
 
 int launch_block_tables(const vector_blocks& v, int32_t* table, int32_t* live, int64_t* slots, int64_t n_slots, int32_t* counts, hipStream_t stream) {
   TableParams p = {};
-  p.held = v.len_held; p.len = v.len; p.free_blocks = v.free_blocks;
+  p.held = v.len_held; p.len = v.len; p.free_blocks = v.free_blocks; p.used = v.n_used;
   p.table = table; p.live = live; p.counts = counts; p.slots = n_slots > 0 ? slots : nullptr;
   p.B = v.batch; p.H = v.n_kv_heads; p.per_seq = v.blocks_per_seq; p.n_free = v.n_free; p.n_slots = (int)n_slots;
   while ((1 << p.shift) < v.block_rows) ++p.shift;

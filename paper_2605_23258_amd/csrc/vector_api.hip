@@ -602,9 +602,10 @@ int vector_block_tables(const vector_blocks* b, int32_t* block_table, int32_t* l
   if (!b || !b->len || !block_table || !len_live || !counts) return VECTOR_ERR_ARG;
   if (b->batch < 1 || b->batch > vec::kMaxRequests || b->n_kv_heads < 1 || b->n_kv_heads > 65535) return VECTOR_ERR_SHAPE;
   if (b->block_rows < 16 || (b->block_rows & (b->block_rows - 1)) || b->blocks_per_seq < 1 || b->n_free < 0) return VECTOR_ERR_ARG;
-  if ((int64_t)b->batch * b->n_kv_heads > INT32_MAX / b->blocks_per_seq) return VECTOR_ERR_SHAPE;
+  const int64_t pairs = (int64_t)b->batch * b->n_kv_heads;
+  if (pairs > (1 << 26) || pairs > INT32_MAX / b->blocks_per_seq) return VECTOR_ERR_SHAPE;     // a launch has fewer than 2^32 threads
   if (n_slots < 0 || n_slots >= INT32_MAX || (!slots && n_slots > 0)) return VECTOR_ERR_ARG;
-  if (len_live == b->len || len_live == b->len_held) return VECTOR_ERR_ARG;
+  if (len_live == b->len || len_live == b->len_held || counts == b->n_used) return VECTOR_ERR_ARG;
   return vec::launch_block_tables(*b, block_table, len_live, slots, n_slots, counts, (hipStream_t)stream);
 }
 
@@ -631,6 +632,7 @@ int vector_store_fp4(const vector_shape* s, const void* k, const void* v, const 
   if (s->seq_len > 1) any_length.seq_len = 1;
   int rc = check_shape(&any_length, false);
   if (rc) return rc;
+  if (s->seq_len >= (1 << 29)) return VECTOR_ERR_SHAPE;      // a launch has fewer than 2^32 threads
   if (!k || !slots || pool_rows < 0 || !aligned16(k) || !aligned16(v) || !fp4_rows_ok(k_pool, k_pool_scale)) return VECTOR_ERR_ARG;
   if (v ? !fp4_rows_ok(v_pool, v_pool_scale) : (v_pool || v_pool_scale)) return VECTOR_ERR_ARG;
   const vec::Fp4Rows rows = {k, v, nullptr, nullptr, slots, s->seq_len, 0, 0, pool_rows, k_pool, k_pool_scale, v_pool, v_pool_scale, nullptr, nullptr};
@@ -640,7 +642,7 @@ int vector_store_fp4(const vector_shape* s, const void* k, const void* v, const 
 int vector_load_fp4(int64_t n_rows, int32_t head_dim, int32_t dtype, const uint8_t* codes, const uint8_t* scales, int64_t pool_rows,
                     const int64_t* slots, void* out, void* stream) {
   if (dtype != VECTOR_F32 && dtype != VECTOR_BF16) return VECTOR_ERR_DTYPE;
-  if ((head_dim != 64 && head_dim != 128) || n_rows > ((int64_t)1 << 34)) return VECTOR_ERR_SHAPE;
+  if ((head_dim != 64 && head_dim != 128) || n_rows >= (1 << 30)) return VECTOR_ERR_SHAPE;
   if (n_rows < 0 || pool_rows < 0 || !out || !aligned16(out) || !fp4_rows_ok(codes, scales)) return VECTOR_ERR_ARG;
   if (n_rows == 0) return VECTOR_OK;
   return vec::launch_load_fp4(n_rows, head_dim, dtype, codes, scales, pool_rows, slots, out, (hipStream_t)stream);

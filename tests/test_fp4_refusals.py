@@ -16,7 +16,7 @@ def shape(**kw):
 
 
 def test_struct_layouts():
-    assert C.sizeof(vb.Blocks) == 6 * 4 + 3 * 8
+    assert C.sizeof(vb.Blocks) == 6 * 4 + 4 * 8
     assert C.sizeof(vb.CacheFp4) == 8 * 4 + 8 * 8 + 4 * 8 + 8 + 4 * 4
 
 
@@ -29,7 +29,8 @@ def blocks(**kw):
 @pytest.mark.parametrize("kw,code", [
     (dict(batch=0), SHAPE), (dict(batch=4097), SHAPE), (dict(n_kv_heads=0), SHAPE), (dict(n_kv_heads=65536), SHAPE), (dict(block_rows=8), ARG),
     (dict(block_rows=24), ARG), (dict(block_rows=-16), ARG), (dict(blocks_per_seq=0), ARG), (dict(n_free=-1), ARG), (dict(len=None), ARG),
-    (dict(batch=4096, n_kv_heads=1024, blocks_per_seq=512), SHAPE), (dict(len=2 * SOME), ARG), (dict(len_held=2 * SOME), ARG)])
+    (dict(batch=4096, n_kv_heads=1024, blocks_per_seq=512), SHAPE), (dict(len=2 * SOME), ARG), (dict(len_held=2 * SOME), ARG),
+    (dict(n_used=SOME), ARG), (dict(batch=4096, n_kv_heads=16385, blocks_per_seq=1), SHAPE)])
 def test_block_tables(kw, code):
     assert vb.lib().vector_block_tables(C.byref(blocks(**kw)), SOME, 2 * SOME, None, 0, SOME, None) == code
 
@@ -75,12 +76,13 @@ def test_store():
         args[i] = bad
         assert L.vector_store_fp4(C.byref(s), *args, None) == ARG, (i, bad)
     assert L.vector_store_fp4(None, *good, None) == ARG
+    assert L.vector_store_fp4(C.byref(shape(seq_len=1 << 29)), *good, None) == SHAPE
 
 
 def test_load():
     L = vb.lib()
     good = [5, 128, vb.VECTOR_BF16, SOME, SOME, 10, None, SOME]
-    for i, bad, code in [(0, -1, ARG), (0, (1 << 34) + 1, SHAPE), (1, 32, SHAPE), (2, 2, DTYPE), (3, None, ARG), (3, SOME + 4, ARG), (4, None, ARG), (4, SOME + 4, ARG), (5, -1, ARG),
+    for i, bad, code in [(0, -1, ARG), (0, 1 << 30, SHAPE), (1, 32, SHAPE), (2, 2, DTYPE), (3, None, ARG), (3, SOME + 4, ARG), (4, None, ARG), (4, SOME + 4, ARG), (5, -1, ARG),
                          (7, None, ARG), (7, SOME + 8, ARG)]:
         args = list(good)
         args[i] = bad

@@ -124,3 +124,23 @@ def test_replays_and_another_stream():
         for g, w in zip((table, live, slots), want):
             assert np.array_equal(g.cpu().numpy(), w)
         assert tuple(counts.tolist()) == want[3]
+
+
+@pytest.mark.parametrize("listed", [True, False])
+def test_blocks_taken_before(listed):
+    """Ids from behind those that calls before have taken; a number out of range is the nearest one in it."""
+    for used, start in ((0, 0), (5, 5), (12, 12), (40, 30), (-3, 0)):
+        ids = list(range(900, 930)) if listed else list(range(30))
+        length, n_used = dev([40, 3, 0, 33]), dev([used])
+        free = dev(ids)
+        b = vb.make_blocks(length, 2, 16, 4, free, used=n_used)
+        if not listed:
+            b.free_blocks = None
+        table, live, counts = torch.full((4, 2, 4), -7, dtype=torch.int32, device=DEV), torch.empty(4, dtype=torch.int32, device=DEV), torch.empty(3, dtype=torch.int32, device=DEV)
+        slots = torch.empty(2, 76, dtype=torch.int64, device=DEV)
+        vb.vector_block_tables(b, table, live, slots, counts)
+        torch.cuda.synchronize()
+        want = fo.block_tables([40, 3, 0, 33], 2, 16, 4, ids[start:], n_slots=76)
+        for g, w in zip((table, live, slots), want):
+            assert np.array_equal(g.cpu().numpy(), w)
+        assert tuple(counts.tolist()) == want[3] and n_used.tolist() == [used]

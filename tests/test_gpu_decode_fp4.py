@@ -414,3 +414,103 @@ def test_sequences_of_different_lengths(d, G, rope, layout):
     if layout == "sequences":
         p.cache.cap_retain, p.cache.n_approx = 1 << 20, max(apx)
     p.check(True, layout)
+
+
+def test_queries_that_are_not_finite_stay_in_their_head():
+    for bad in (float("inf"), float("nan"), float("-inf")):
+        for d, G in ((128, 4), (128, 7), (128, 12), (64, 4)):
+            p = Problem([60, 5], 40, d=d, G=G)
+            p.q_dev[1, G + 1, 17] = bad
+            got = p.call().cpu().numpy()
+            want, tol = p.expected()
+            assert np.isnan(got[1, G + 1]).all()
+            got[1, G + 1] = want[1, G + 1]
+            assert (np.abs(got - want) <= tol).all()
+
+
+def test_rows_far_into_a_pool():
+    """Pools of 2^26 + 64 rows, 4 GiB of codes each: blocks that begin beyond 2^32 bytes, and the step's row among them."""
+    small = Problem([70, 33], 0, layout="paged", block_rows=32, room=20)
+    rows = (1 << 26) + 64 * 8
+    big = Problem([70, 33], 0, layout="paged", block_rows=32, room=20)
+    first = (1 << 26) // 32 - 6
+    pools = []
+    for codes, scales in small.pools[:2]:
+        c, s = torch.zeros(rows, 64, dtype=torch.uint8, device=DEV), torch.zeros(rows, 4, dtype=torch.uint8, device=DEV)
+        at = slice(first * 32, first * 32 + codes.shape[0])
+        c[at], s[at] = codes, scales
+        pools.append((c, s))
+    big.table_dev.copy_(dev(small.table + first))
+    big.cache.n_blocks = rows // 32
+    (big.cache.k_ret, big.cache.k_ret_scale), (big.cache.v_ret, big.cache.v_ret_scale) = ((c.data_ptr(), s.data_ptr()) for c, s in pools)
+    want, got = small.call(True), big.call(True)
+    torch.cuda.synchronize()
+    assert torch.equal(want, got)
+    for (c, s), (c2, s2) in zip(small.pools[:2], pools):
+        at = slice(first * 32, first * 32 + c.shape[0])
+        assert torch.equal(c, c2[at]) and torch.equal(s, s2[at])
+    # the same rows in one contiguous segment that begins beyond 2^32 bytes
+    far = Problem([70], [0], H=1, layout="sequences", caps=[100])
+    start = (1 << 26) + 7
+    moved = []
+    for codes, scales in far.pools[:2]:
+        c, s = torch.zeros(rows, 64, dtype=torch.uint8, device=DEV), torch.zeros(rows, 4, dtype=torch.uint8, device=DEV)
+        c[start:start + 100], s[start:start + 100] = codes, scales
+        moved.append((c, s))
+    want = far.call()
+    far.keep[2].fill_(start)
+    (far.cache.k_ret, far.cache.k_ret_scale), (far.cache.v_ret, far.cache.v_ret_scale) = ((c.data_ptr(), s.data_ptr()) for c, s in moved)
+    assert torch.equal(want, far.call())
+
+
+def test_a_captured_serving_loop_without_the_host():
+    """Blocks for the next tokens and the step over them in one graph, replayed: lengths, tables and the place in the free list advance on the
+    GPU.  Against the same calls made eagerly."""
+    rng = np.random.default_rng(4)
+    H, G, d, R, per_seq, B, steps = 2, 4, 128, 16, 6, 5, 24
+    half = lambda *s: dev(dg.f32_to_bf16_bits(rng.standard_normal(s).astype(np.float32)).view(np.int16)).view(torch.bfloat16)
+    n_blocks = B * H * per_seq
+    free = dev(rng.permutation(n_blocks).astype(np.int32))
+    tokens = [(half(B, H * G, d), half(B, H, d), half(B, H, d)) for _ in range(steps)]
+
+    class Loop:
+        def __init__(self):
+            i32 = lambda *s: torch.zeros(*s, dtype=torch.int32, device=DEV)
+            self.pool = [torch.full((n_blocks * R, n), 255, dtype=torch.uint8, device=DEV) for n in (d // 2, d // 32, d // 2, d // 32)]
+            self.table, self.live, self.held, self.wanted, self.grown, self.counts, self.used = i32(B, H, per_seq), i32(B), i32(B), i32(B), i32(B), i32(3), i32(1)
+            self.q, self.k, self.v = (torch.zeros_like(x) for x in tokens[0])
+            self.out = torch.zeros(B, H * G, d, device=DEV)
+            c = self.cache = vb.CacheFp4(batch=B, n_q_heads=H * G, n_kv_heads=H, head_dim=d, dtype=vb.VECTOR_BF16, cap_retain=per_seq * R, n_approx=0)
+            c.k_ret, c.k_ret_scale, c.v_ret, c.v_ret_scale = (x.data_ptr() for x in self.pool)
+            c.len_retain, c.ret_block_table, c.ret_block_rows, c.ret_blocks_per_seq, c.n_blocks = self.live.data_ptr(), self.table.data_ptr(), R, per_seq, n_blocks
+            self.ws = pl.alloc_workspace(vb.vector_decode_fp4_workspace_bytes(c))
+            self.blocks = vb.make_blocks(self.wanted, H, R, per_seq, free, held=self.held, used=self.used)
+
+        def step(self, stream):
+            self.held.copy_(self.live)
+            torch.add(self.live, 1, out=self.wanted)
+            vb.vector_block_tables(self.blocks, self.table, self.grown, None, self.counts, stream=stream)
+            self.used.add_(self.counts[:1])
+            vb.vector_decode_step_fp4(self.cache, self.q, self.k, self.v, 1 / np.sqrt(d), self.out, self.ws, flags=vb.VECTOR_DECODE_OUT_F32, stream=stream)
+
+    eager, graphed, warm = Loop(), Loop(), Loop()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        warm.step(side)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        graphed.step(torch.cuda.current_stream())
+    for i, token in enumerate(tokens):
+        for loop in (eager, graphed):
+            for to, x in zip((loop.q, loop.k, loop.v), token):
+                to.copy_(x)
+        eager.step(None)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for name in ("out", "live", "table", "used", "grown"):
+            assert torch.equal(getattr(eager, name), getattr(graphed, name)), f"step {i}: {name}"
+        assert eager.live.tolist() == [i + 1] * B and eager.used.item() == B * H * (-(-(i + 1) // R))
