@@ -7,7 +7,7 @@
 // An element in 4 bits times its scale has two significant bits and is a bf16 number exactly; the weights go in as parts of eight bits each.
 //
 // A wave takes 32 rows at a time and waits for no other before the end.  Their codes and scales go from memory straight into a ring of its
-// own in LDS (Fp4Stage), past the caches (16 whole caches of 32768 tokens 105 us with them, 91 without: 6.2 TB/s), so that what is on its way
+// own in LDS (Fp4Stage), past the caches (16 whole caches of 32768 tokens 105 us with them, 90 without: 6.3 TB/s), so that what is on its way
 // takes no registers, and are read back in the matrix cores' order:
 //   scores   S[t][g] = sum_e K[t][e] q[g][e]      A = K: lane (m, quarter) holds D / 4 consecutive elements of a row, which is one read and
 //                                                  one scale.  128 dims: as they are, in 4 bits with their scales, against query rows in
@@ -42,18 +42,14 @@ struct Fp4Params {
 constexpr int kFp4TileRows = 32;
 constexpr float kRaiseAt = 16.f;       // log2: how far a score may lie above its column's reference before that is raised
 
-// no more than n loads on their way; n is the same for the wave
+// no more than n loads on their way, those of a tile or none; n is the same for the wave
 __device__ __forceinline__ void wait_tiles(int n) {
   switch (n) {
     case 0: wait_loads<0>(); break;
     case 2: wait_loads<2>(); break;
     case 3: wait_loads<3>(); break;
-    case 4: wait_loads<4>(); break;
     case 5: wait_loads<5>(); break;
-    case 6: wait_loads<6>(); break;
     case 9: wait_loads<9>(); break;
-    case 10: wait_loads<10>(); break;
-    case 18: wait_loads<18>(); break;
     default: wait_loads<0>();
   }
 }
@@ -80,7 +76,10 @@ template <int D> struct Fp4Stage {
   static __device__ __forceinline__ int twist(int place) { return D == 128 ? (place >> 2) & 3 : (place >> 3) & 1; }
   static __device__ __forceinline__ int piece(int row, int piece) { return place(row) * kCode + ((piece ^ twist(place(row))) * 16); }
 };
-constexpr int kFp4Stages = 3;
+// Tiles of a wave: one on its way while one is worked on.  Split launch, us, two stages / three / four (two workgroups per CU) / two and four workgroups:
+// 16 routed sequences of 32768 tokens 18.9 / 19.8 / 21.3 / 21.2, 24 unequal ones 14.0 / 16.1 / 18.3 / 14.7, on rotated keys 20.7 / 22.9 / 33.4 / 28.1,
+// 64 whole ones of 2048 28.3 / 31.1 / 35.0 / 28.0, 16 whole ones of 32768 90.1 / 91.3 / 92.1 / 90.8.
+constexpr int kFp4Stages = 2;
 
 // Rows of a workgroup: of the retained segment, or approximated ones, as they are or turned back with pairs (x[i], x[i + D / 2]) or
 // (x[2 i], x[2 i + 1]).
@@ -507,11 +506,10 @@ __device__ __forceinline__ void attend_fp4(const Fp4Params& f, const RopeParams&
 
   // loads of a tile; of tiles that went by the other way there are none on their way, nor of any before these
   const int per_tile = is_apx ? St::kLoads + 1 + (D == 64 && turned && positions ? 1 : 0) : (small_blocks ? 4 : 2) * St::kLoads + 1;
-  static_assert(kFp4Stages == 3, "two tiles on their way while one is worked on");
   const int tiles = row_begin + wave * kFp4TileRows < row_end ? (row_end - row_begin - wave * kFp4TileRows + kStepRows - 1) / kStepRows : 0;
   const int first = row_begin + wave * kFp4TileRows;
+  static_assert(kFp4Stages == 2, "one tile on its way");
   if (tiles > 0) fill(first, ring);
-  if (tiles > 1) fill(first + kStepRows, ring + St::kBytes);
   // the query rows in operand order; the first tiles are on their way
   if constexpr (kMx) {
     // A row in two fp8 parts under a scale for every 32 dims: four bits and the four behind them, all that bf16 has; an element far below its
@@ -596,11 +594,11 @@ __device__ __forceinline__ void attend_fp4(const Fp4Params& f, const RopeParams&
     const int base = first + i * kStepRows;
     // the stage of the tile before is free: what was read of it is in registers
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    if (i + 2 < tiles) fill(base + 2 * kStepRows, ring + (stage == 0 ? 2 : stage - 1) * St::kBytes);
-    wait_tiles(per_tile * min(2, tiles - 1 - i));
+    if (i + 1 < tiles) fill(base + kStepRows, ring + (1 - stage) * St::kBytes);
+    wait_tiles(i + 1 < tiles ? per_tile : 0);
     wave_fence();
     consume(ring + stage * St::kBytes, base);
-    stage = stage == 2 ? 0 : stage + 1;
+    stage = 1 - stage;
   }
 
   // ---- merge the waves ----
