@@ -657,8 +657,15 @@ __device__ __forceinline__ void attend_fp4(const Fp4Params& f, const RopeParams&
   }
 }
 
+// Workgroups per CU.  fp32 turned back at 128 dims needs more than the 168 registers of three: with three 49 are spilled, and 8 sequences of 16384 tokens
+// take 23.9 us, with two 19.3.
+template <typename T, int D, Fp4RowKind APPROX>
+constexpr int fp4_per_cu() {
+  return sizeof(T) == 4 && D == 128 && APPROX != Fp4RowKind::kApprox ? 2 : kFp4PerCu;
+}
+
 template <typename T, int D, int COLS, Fp4RowKind APPROX>
-__global__ __launch_bounds__(DT_, 3) void decode_split_fp4_kernel(Fp4Params f, RopeParams rp) {
+__global__ __launch_bounds__(DT_, (fp4_per_cu<T, D, APPROX>())) void decode_split_fp4_kernel(Fp4Params f, RopeParams rp) {
   const SplitRows r = grid_split<DW * kFp4TileRows>(f.d);
   if (r.is_apx) attend_fp4<T, D, COLS, APPROX>(f, rp, r, (int)threadIdx.x);
   else attend_fp4<T, D, COLS, Fp4RowKind::kRetained>(f, rp, r, (int)threadIdx.x);
@@ -677,7 +684,9 @@ int launch_split_fp4(const Fp4Params& f, const RopeParams* rope, hipStream_t str
 
 template <typename T, int D, int COLS>
 int run_split_fp4(Fp4Params& f, const RopeParams* rope, hipStream_t stream) {
-  pick_splits_fp4(f.d.B, f.d.Hkv, f.d.cap_retain, f.d.n_approx, rope ? kFp4Turned : kFp4Approx, f.d.splits_ret, f.d.splits_apx);
+  pick_splits_fp4(f.d.B, f.d.Hkv, f.d.cap_retain, f.d.n_approx, rope ? kFp4Turned : kFp4Approx,
+                  rope ? fp4_per_cu<T, D, Fp4RowKind::kTurnedApart>() : fp4_per_cu<T, D, Fp4RowKind::kApprox>(),
+                  f.d.splits_ret, f.d.splits_apx);
   if (!rope || f.d.n_approx == 0) return launch_split_fp4<T, D, COLS, Fp4RowKind::kApprox>(f, nullptr, stream);
   return rope->interleaved ? launch_split_fp4<T, D, COLS, Fp4RowKind::kTurnedNext>(f, rope, stream)
                            : launch_split_fp4<T, D, COLS, Fp4RowKind::kTurnedApart>(f, rope, stream);

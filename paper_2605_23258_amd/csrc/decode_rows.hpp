@@ -164,7 +164,7 @@ inline bool pick_one_round(const SplitCosts& c, int batch, int n_kv_heads, int c
   return best >= 0.0;
 }
 
-// Caches held in 4 bits: as many workgroups as run at the same time, cut so that the longest piece is the shortest; steps of 128 rows.
+// Caches held in 4 bits: as many workgroups as run at the same time, per_cu on a CU, cut so that the longest piece is the shortest; steps of 128 rows.
 // What a step of approximated rows takes, in steps of retained ones: they have half the bytes, but as much arithmetic, and sines and cosines
 // where they are turned back.  Split launch, us, equal pieces / these: 24 unequal sequences of up to 16000 tokens on rotated keys 26.3 / 22.0;
 // 16 of 32768 33.4 / 33.1, on plain keys 21.6 / 21.4, four 11.7 / 11.3.  More workgroups than run at the same time (1024, 1536, 2304) are slower: 16 of
@@ -172,9 +172,9 @@ inline bool pick_one_round(const SplitCosts& c, int batch, int n_kv_heads, int c
 // done its short pieces leaves the memory to the others: 24 unequal ones 17.4 / 18.2, 48 of up to 4000 19.2 / 23.0.
 constexpr int kFp4StepRows = 128, kFp4PerCu = 3;
 constexpr double kFp4Approx = 0.8, kFp4Turned = 2.5;
-inline void pick_splits_fp4(int batch, int n_kv_heads, int cap_retain, int n_approx, double apx_cost, int& s_ret, int& s_apx) {
+inline void pick_splits_fp4(int batch, int n_kv_heads, int cap_retain, int n_approx, double apx_cost, int per_cu, int& s_ret, int& s_apx) {
   const int64_t steps_r = ((int64_t)cap_retain + kFp4StepRows - 1) / kFp4StepRows, steps_a = ((int64_t)n_approx + kFp4StepRows - 1) / kFp4StepRows;
-  const int64_t pairs = (int64_t)batch * n_kv_heads, at_once = 256 * kFp4PerCu;
+  const int64_t pairs = (int64_t)batch * n_kv_heads, at_once = 256 * per_cu;
   const int most = (int)std::max<int64_t>(2, std::min<int64_t>(kMaxSplits, at_once / pairs));
   s_ret = steps_r > 0 || steps_a == 0 ? 1 : 0;   // nothing cached: one workgroup writes the empty partial
   s_apx = steps_a > 0 ? 1 : 0;
