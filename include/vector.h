@@ -453,18 +453,19 @@ VECTOR_API int vector_compact_fp4(const vector_shape* shape, const void* k, cons
 /* Rows into pools of rows in 4 bits by slots (those of vector_block_tables, or any others): row t of KV head h of k (and of v,
  * which may be NULL with its pool) goes to row slots[h * seq_len + t] of the pools, which have pool_rows rows.  A row whose slot is
  * negative or not below pool_rows goes nowhere.  Slots must differ.  k, v: [Hkv, seq_len, d] with the shape's strides and dtype;
- * slots: device [Hkv, seq_len].  seq_len may be up to 2^29 - 1 here (VECTOR_ERR_SHAPE beyond). */
+ * slots: device [Hkv, seq_len].  seq_len may be up to 2^28 here (VECTOR_ERR_SHAPE beyond). */
 VECTOR_API int vector_store_fp4(const vector_shape* shape, const void* k, const void* v, const int64_t* slots, int64_t pool_rows,
                      uint8_t* k_pool, uint8_t* k_pool_scale, uint8_t* v_pool, uint8_t* v_pool_scale, void* stream);
 
 /* The values of rows in 4 bits: out[r] (device [n_rows, head_dim] of dtype) is row slots[r] of an array of pool_rows rows, row r where
- * slots is NULL; zeros where there is no such row.  The values are exact in either type.  VECTOR_ERR_SHAPE for 2^30 rows
- * or more. */
+ * slots is NULL; zeros where there is no such row.  The values are exact in either type.  VECTOR_ERR_SHAPE for more than
+ * 2^29 rows. */
 VECTOR_API int vector_load_fp4(int64_t n_rows, int32_t head_dim, int32_t dtype, const uint8_t* codes, const uint8_t* scales,
                     int64_t pool_rows, const int64_t* slots, void* out, void* stream);
 
 /* vector_cache with its rows in 4 bits.  Everything is laid out as there, in rows of codes and rows of scales: k_ret, k_ret_scale
- * [batch, Hkv, cap_retain, ..] and so on; dtype is that of q, W, out and the step's token. */
+ * [batch, Hkv, cap_retain, ..] and so on; dtype is that of q, W, out and the step's token.
+ * cap_retain and n_approx, and those of every sequence: up to 2^30 (VECTOR_ERR_SHAPE beyond). */
 typedef struct {
   int32_t batch, n_q_heads, n_kv_heads, head_dim;
   int32_t dtype;

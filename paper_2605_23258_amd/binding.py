@@ -110,9 +110,11 @@ class Blocks(C.Structure):
 
 
 def make_blocks(length, n_kv_heads: int, block_rows: int, blocks_per_seq: int, free, held=None, used=None) -> Blocks:
-    """Blocks from device int32 tensors: lengths asked for, ids of free blocks, the lengths that the requests hold blocks for (None:
-    all requests are new), and how many of the ids have been taken from the front (None: none).  The tensors have to outlive it."""
-    return Blocks(batch=length.numel(), n_kv_heads=n_kv_heads, block_rows=block_rows, blocks_per_seq=blocks_per_seq, n_free=free.numel(),
+    """Blocks from device int32 tensors: lengths asked for, ids of free blocks (or a number: so many, 0, 1, 2, ..), the lengths that the requests
+    hold blocks for (None: all requests are new), and how many of the ids have been taken from the front (None: none).  The tensors
+    have to outlive it."""
+    n_free, free = (free, None) if isinstance(free, int) else (free.numel(), free)
+    return Blocks(batch=length.numel(), n_kv_heads=n_kv_heads, block_rows=block_rows, blocks_per_seq=blocks_per_seq, n_free=n_free,
                   len_held=_ptr(held), len=_ptr(length), free_blocks=_ptr(free), n_used=_ptr(used))
 
 

@@ -100,8 +100,9 @@ __global__ __launch_bounds__(kThreads) void block_tables_kernel(TableParams p) {
 
   if ((int)blockIdx.x < p.slot_groups) {
     // slots: a thread takes two tokens for all KV heads; neighbours are tokens of one request, mostly
-    const int t0 = blockIdx.x * kTokensPerGroup;
-    for (int t = t0 + 2 * tid; t < min(t0 + kTokensPerGroup, p.n_slots); t += 2 * kThreads) {
+    static_assert(kTokensPerGroup == 2 * kThreads, "one pair a thread");
+    const int t = (int)blockIdx.x * kTokensPerGroup + 2 * tid;         // below 2^31: n_slots is, and of no more groups than it takes
+    if (t < p.n_slots) {
       // the request b with tokens[b] <= t < tokens[b + 1]
       int lo = 0, hi = p.B;                  // tokens[lo] <= t; hi == B or t < tokens[hi]
       while (hi - lo > 1) {
@@ -201,7 +202,7 @@ int launch_block_tables(const vector_blocks& v, int32_t* table, int32_t* live, i
   p.table = table; p.live = live; p.counts = counts; p.slots = n_slots > 0 ? slots : nullptr;
   p.B = v.batch; p.H = v.n_kv_heads; p.per_seq = v.blocks_per_seq; p.n_free = v.n_free; p.n_slots = (int)n_slots;
   while ((1 << p.shift) < v.block_rows) ++p.shift;
-  p.slot_groups = (p.n_slots + kTokensPerGroup - 1) / kTokensPerGroup;
+  p.slot_groups = (int)((n_slots + kTokensPerGroup - 1) / kTokensPerGroup);
   const int table_groups = (p.B * p.H + kPairsPerGroup - 1) / kPairsPerGroup;
   const size_t lds = 2 * (p.B + 1) * sizeof(int) + p.B * sizeof(Request);
   VEC_HIP(set_max_lds(reinterpret_cast<const void*>(block_tables_kernel), lds));

@@ -632,7 +632,7 @@ int vector_store_fp4(const vector_shape* s, const void* k, const void* v, const 
   if (s->seq_len > 1) any_length.seq_len = 1;
   int rc = check_shape(&any_length, false);
   if (rc) return rc;
-  if (s->seq_len >= (1 << 29)) return VECTOR_ERR_SHAPE;      // a launch has fewer than 2^32 threads
+  if (s->seq_len > (1 << 28)) return VECTOR_ERR_SHAPE;       // a launch has fewer than 2^32 threads
   if (!k || !slots || pool_rows < 0 || !aligned16(k) || !aligned16(v) || !fp4_rows_ok(k_pool, k_pool_scale)) return VECTOR_ERR_ARG;
   if (v ? !fp4_rows_ok(v_pool, v_pool_scale) : (v_pool || v_pool_scale)) return VECTOR_ERR_ARG;
   const vec::Fp4Rows rows = {k, v, nullptr, nullptr, slots, s->seq_len, 0, 0, pool_rows, k_pool, k_pool_scale, v_pool, v_pool_scale, nullptr, nullptr};
@@ -642,7 +642,7 @@ int vector_store_fp4(const vector_shape* s, const void* k, const void* v, const 
 int vector_load_fp4(int64_t n_rows, int32_t head_dim, int32_t dtype, const uint8_t* codes, const uint8_t* scales, int64_t pool_rows,
                     const int64_t* slots, void* out, void* stream) {
   if (dtype != VECTOR_F32 && dtype != VECTOR_BF16) return VECTOR_ERR_DTYPE;
-  if ((head_dim != 64 && head_dim != 128) || n_rows >= (1 << 30)) return VECTOR_ERR_SHAPE;
+  if ((head_dim != 64 && head_dim != 128) || n_rows > (1 << 29)) return VECTOR_ERR_SHAPE;
   if (n_rows < 0 || pool_rows < 0 || !out || !aligned16(out) || !fp4_rows_ok(codes, scales)) return VECTOR_ERR_ARG;
   if (n_rows == 0) return VECTOR_OK;
   return vec::launch_load_fp4(n_rows, head_dim, dtype, codes, scales, pool_rows, slots, out, (hipStream_t)stream);
@@ -657,6 +657,7 @@ static int check_fp4_cache(const vector_cache_fp4* c) {
   if (c->n_q_heads < c->n_kv_heads || c->n_q_heads % c->n_kv_heads) return VECTOR_ERR_SHAPE;
   const int G = c->n_q_heads / c->n_kv_heads;
   if (G > 8 && G != 10 && G != 12 && G != 16) return VECTOR_ERR_SHAPE;
+  if (c->cap_retain > (1 << 30) || c->n_approx > (1 << 30)) return VECTOR_ERR_SHAPE;           // rows and steps behind them are ints
   return c->cap_retain < 0 || c->n_approx < 0 ? VECTOR_ERR_ARG : VECTOR_OK;
 }
 

@@ -76,13 +76,13 @@ def test_store():
         args[i] = bad
         assert L.vector_store_fp4(C.byref(s), *args, None) == ARG, (i, bad)
     assert L.vector_store_fp4(None, *good, None) == ARG
-    assert L.vector_store_fp4(C.byref(shape(seq_len=1 << 29)), *good, None) == SHAPE
+    assert L.vector_store_fp4(C.byref(shape(seq_len=(1 << 28) + 1)), *good, None) == SHAPE
 
 
 def test_load():
     L = vb.lib()
     good = [5, 128, vb.VECTOR_BF16, SOME, SOME, 10, None, SOME]
-    for i, bad, code in [(0, -1, ARG), (0, 1 << 30, SHAPE), (1, 32, SHAPE), (2, 2, DTYPE), (3, None, ARG), (3, SOME + 4, ARG), (4, None, ARG), (4, SOME + 4, ARG), (5, -1, ARG),
+    for i, bad, code in [(0, -1, ARG), (0, (1 << 29) + 1, SHAPE), (1, 32, SHAPE), (2, 2, DTYPE), (3, None, ARG), (3, SOME + 4, ARG), (4, None, ARG), (4, SOME + 4, ARG), (5, -1, ARG),
                          (7, None, ARG), (7, SOME + 8, ARG)]:
         args = list(good)
         args[i] = bad
@@ -107,7 +107,8 @@ def step(c, k_new=SOME, v_new=SOME):
 
 @pytest.mark.parametrize("kw,code", [
     (dict(batch=0), SHAPE), (dict(batch=65536), SHAPE), (dict(n_q_heads=9), SHAPE), (dict(n_q_heads=22), SHAPE), (dict(n_q_heads=1), SHAPE), (dict(head_dim=96), SHAPE),
-    (dict(dtype=3), DTYPE), (dict(cap_retain=-1), ARG), (dict(n_approx=-1), ARG)])
+    (dict(dtype=3), DTYPE), (dict(cap_retain=-1), ARG), (dict(n_approx=-1), ARG),
+    (dict(cap_retain=(1 << 30) + 1), SHAPE), (dict(n_approx=(1 << 30) + 1), SHAPE)])
 def test_cache_shapes(kw, code):
     c = cache(**kw)
     assert attn(c) == code and step(c) == code and vb.vector_decode_fp4_workspace_bytes(c) == 0

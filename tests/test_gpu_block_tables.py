@@ -93,6 +93,22 @@ def test_ids_whose_rows_pass_32_bits():
     assert got[2].tolist() == [[(1 << 37) + i for i in range(5)]]
 
 
+def test_longest_slot_map():
+    """As many columns as there may be, 16 GiB of them; a request that does not fit the last two."""
+    n_slots, R = 2 ** 31 - 2, 1 << 20
+    length = dev([2 ** 30, 2 ** 30 - 7, 3, 5])
+    table, live, counts = torch.full((4, 1, 1024), -7, dtype=torch.int32, device=DEV), torch.empty(4, dtype=torch.int32, device=DEV), torch.empty(3, dtype=torch.int32, device=DEV)
+    slots = torch.full((1, n_slots), -7, dtype=torch.int64, device=DEV)
+    vb.vector_block_tables(vb.make_blocks(length, 1, R, 1024, 3000), table, live, slots, counts)
+    torch.cuda.synchronize()
+    assert live.tolist() == [2 ** 30, 2 ** 30 - 7, 3, 0] and counts.tolist() == [2049, 2050, 2 ** 31 - 1]
+    full, part = 2 ** 31 - 7, 1 << 28
+    for a in range(0, full, part):
+        b = min(a + part, full)
+        assert bool((slots[0, a:b] == torch.arange(a, b, device=DEV)).all()), a
+    assert slots[0, full:].tolist() == [2 ** 31, 2 ** 31 + 1, 2 ** 31 + 2, -1, -1]
+
+
 def test_replays_and_another_stream():
     """A captured call reads the lengths that the buffers hold then."""
     B, H, R, per_seq = 50, 4, 16, 12
