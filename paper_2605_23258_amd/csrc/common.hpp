@@ -300,11 +300,15 @@ struct RopeParams {
   int32_t interleaved;                   // 0: pair i = (x[i], x[i + d/2]); 1: pair i = (x[2i], x[2i + 1])
 };
 
-// (cos, sin) of position * frequency; pos_f = the position as a float (exact below 2^24)
-__device__ __forceinline__ void rotary_cos_sin(float pos_f, float t_hi, float t_lo, float& c, float& s) {
+// position * frequency in turns, whole ones left out; pos_f = the position as a float (exact below 2^24)
+__device__ __forceinline__ float rotary_turns(float pos_f, float t_hi, float t_lo) {
   const float p = pos_f * t_hi;
   const float err = fmaf(pos_f, t_hi, -p);                 // exact: the bits the product dropped
-  const float u = __builtin_amdgcn_fractf(p) + fmaf(pos_f, t_lo, err);
+  return __builtin_amdgcn_fractf(p) + fmaf(pos_f, t_lo, err);
+}
+// (cos, sin) of it
+__device__ __forceinline__ void rotary_cos_sin(float pos_f, float t_hi, float t_lo, float& c, float& s) {
+  const float u = rotary_turns(pos_f, t_hi, t_lo);
   c = __builtin_amdgcn_cosf(u);
   s = __builtin_amdgcn_sinf(u);
 }

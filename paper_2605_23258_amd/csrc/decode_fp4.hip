@@ -40,6 +40,12 @@ struct Fp4Params {
 };
 
 constexpr int kFp4TileRows = 32;
+// Keys turned back by near positions.  The turns of a lane's eight rows are those of the first one and the difference, one operation instead
+// of five, as long as no pair turns more than this between them.  That is off by 2^-18 turns (the rounding of a number below 128) and 2^-19 (the
+// frequency's, 2^-25 of it), 3.6e-5 of the pair's length, before the row is rounded to bf16, 2^-8; fp32 does not take it.
+// More than four query heads do not either: their registers do not hold both ways (eight 31.0 us with it, 29.8 without; sixteen 26.0, 22.5).
+// Split launch, us, without / with: 16 sequences of 32768 tokens 31.6 / 27.5, four 15.0 / 13.2, 24 unequal ones 21.4 / 19.4, 64 dims 22.8 / 20.5.
+constexpr float kNearTurns = 64.f;
 constexpr float kRaiseAt = 16.f;       // log2: how far a score may lie above its column's reference before that is raised
 
 // no more than n loads on their way, those of a tile or none; n is the same for the wave
@@ -470,36 +476,72 @@ __device__ __forceinline__ void attend_fp4(const Fp4Params& f, const RopeParams&
         }
         __builtin_amdgcn_sched_barrier(0);             // all pairs' sines at once would not fit the registers
       };
-      if constexpr (apart) {
-        constexpr int kHalf = kDims / 2;               // pairs of a lane, two a byte of codes
-        for_each_constant<kHalf / 2>([&](auto c) VEC_INLINE {
-          float a[2][8], b[2][8];
+      auto turn = [&](auto near) VEC_INLINE {
+        // (what both ways share would be drawn in front of the branch, too much for the registers)
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const f32x2 x = fp4_pair_f32<decltype(c)::value>(r[j], exponent(bytes[j], to_exponent));
-            const f32x2 y = fp4_pair_f32<2 + decltype(c)::value>(r[j], exponent(bytes[j], to_exponent + kScale / 2 * 8u));
+        for (int j = 0; j < 8; ++j) {
+          if constexpr (decltype(near)::value) asm volatile("; near" : "+v"(r[j]), "+v"(pos[j]));
+          else asm volatile("; far" : "+v"(r[j]), "+v"(pos[j]));
+        }
+        auto cos_sin = [&](int j, float from, float hi, float lo, float& cs, float& sn) VEC_INLINE {
+          if constexpr (decltype(near)::value) {
+            const float u = j ? fmaf(pos[j], hi, from) : from;
+            cs = __builtin_amdgcn_cosf(u);
+            sn = __builtin_amdgcn_sinf(u);
+          } else {
+            rotary_cos_sin(pos[j], hi, lo, cs, sn);
+          }
+        };
+        auto first_turns = [&](float hi, float lo) VEC_INLINE { return decltype(near)::value ? rotary_turns(pos[0], hi, lo) : 0.f; };
+        if constexpr (apart) {
+          constexpr int kHalf = kDims / 2;               // pairs of a lane, two a byte of codes
+          for_each_constant<kHalf / 2>([&](auto c) VEC_INLINE {
+            float a[2][8], b[2][8];
+            const float from[2] = {first_turns(t_hi[2 * c], t_lo[2 * c]), first_turns(t_hi[2 * c + 1], t_lo[2 * c + 1])};
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              float cs, sn;
-              rotary_cos_sin(pos[j], t_hi[2 * c + e], t_lo[2 * c + e], cs, sn);
-              rotary_back(x[e], y[e], cs, sn, a[e][j], b[e][j]);
+            for (int j = 0; j < 8; ++j) {
+              const f32x2 x = fp4_pair_f32<decltype(c)::value>(r[j], exponent(bytes[j], to_exponent));
+              const f32x2 y = fp4_pair_f32<2 + decltype(c)::value>(r[j], exponent(bytes[j], to_exponent + kScale / 2 * 8u));
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                float cs, sn;
+                cos_sin(j, from[e], t_hi[2 * c + e], t_lo[2 * c + e], cs, sn);
+                rotary_back(x[e], y[e], cs, sn, a[e][j], b[e][j]);
+              }
             }
-          }
-          add(std::integral_constant<int, decltype(c)::value>{}, a[0], a[1]);
-          add(std::integral_constant<int, kHalf / 2 + decltype(c)::value>{}, b[0], b[1]);
-        });
-      } else {
-        for_each_constant<kDims / 2>([&](auto c) VEC_INLINE {
-          float a[8], b[8];
+            add(std::integral_constant<int, decltype(c)::value>{}, a[0], a[1]);
+            add(std::integral_constant<int, kHalf / 2 + decltype(c)::value>{}, b[0], b[1]);
+          });
+        } else {
+          for_each_constant<kDims / 2>([&](auto c) VEC_INLINE {
+            float a[8], b[8];
+            const float from = first_turns(t_hi[c], t_lo[c]);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const f32x2 x = fp4_pair_f32<decltype(c)::value>(r[j], exponent(bytes[j], to_exponent));
-            float cs, sn;
-            rotary_cos_sin(pos[j], t_hi[c], t_lo[c], cs, sn);
-            rotary_back(x[0], x[1], cs, sn, a[j], b[j]);
-          }
-          add(c, a, b);
-        });
+            for (int j = 0; j < 8; ++j) {
+              const f32x2 x = fp4_pair_f32<decltype(c)::value>(r[j], exponent(bytes[j], to_exponent));
+              float cs, sn;
+              cos_sin(j, from, t_hi[c], t_lo[c], cs, sn);
+              rotary_back(x[0], x[1], cs, sn, a[j], b[j]);
+            }
+            add(c, a, b);
+          });
+        }
+      };
+      bool near = false;
+      if constexpr (!kExact && COLS == 4) {
+        float most = 0.f, fastest = fabsf(t_hi[0]);
+#pragma unroll
+        for (int j = 1; j < 8; ++j) most = fmaxf(most, fabsf(pos[j] - pos[0]));
+#pragma unroll
+        for (int e = 1; e < kDims / 2; ++e) fastest = fmaxf(fastest, fabsf(t_hi[e]));
+        near = __ballot(!(most * fastest <= kNearTurns)) == 0;
+      }
+      if (near) {
+#pragma unroll
+        for (int j = 1; j < 8; ++j) pos[j] -= pos[0];
+        turn(std::true_type{});
+      } else {
+        turn(std::false_type{});
       }
     }
   };
@@ -673,7 +715,7 @@ __global__ __launch_bounds__(DT_, (fp4_per_cu<T, D, APPROX>())) void decode_spli
 
 template <typename T, int D, int COLS, Fp4RowKind APPROX>
 int launch_split_fp4(const Fp4Params& f, const RopeParams* rope, hipStream_t stream) {
-  const dim3 grid(f.d.splits_ret + f.d.splits_apx, f.d.Hkv, f.d.B);
+  const dim3 grid = f.d.by_kind ? dim3(f.d.Hkv, f.d.B, f.d.splits_ret + f.d.splits_apx) : dim3(f.d.splits_ret + f.d.splits_apx, f.d.Hkv, f.d.B);
   constexpr int lds = DW * kFp4Stages * Fp4Stage<D>::kBytes;
   constexpr auto kernel = decode_split_fp4_kernel<T, D, COLS, APPROX>;
   VEC_HIP(set_max_lds(reinterpret_cast<const void*>(kernel), lds));
@@ -687,6 +729,9 @@ int run_split_fp4(Fp4Params& f, const RopeParams* rope, hipStream_t stream) {
   pick_splits_fp4(f.d.B, f.d.Hkv, f.d.cap_retain, f.d.n_approx, rope ? kFp4Turned : kFp4Approx,
                   rope ? fp4_per_cu<T, D, Fp4RowKind::kTurnedApart>() : fp4_per_cu<T, D, Fp4RowKind::kApprox>(),
                   f.d.splits_ret, f.d.splits_apx);
+  // Pieces of both kinds of rows on every CU, so that one computes while the other one waits for memory; us, split / head first: 48 unequal sequences of up to
+  // 4000 tokens 16.9 / 15.8, 64 dims on rotated keys 21.8 / 20.6, four sequences 15.0 / 13.6.  One kind: 32 unequal ones of up to 16000 68.9 / 71.8.
+  f.d.by_kind = f.d.splits_ret > 0 && f.d.splits_apx > 0;
   if (!rope || f.d.n_approx == 0) return launch_split_fp4<T, D, COLS, Fp4RowKind::kApprox>(f, nullptr, stream);
   return rope->interleaved ? launch_split_fp4<T, D, COLS, Fp4RowKind::kTurnedNext>(f, rope, stream)
                            : launch_split_fp4<T, D, COLS, Fp4RowKind::kTurnedApart>(f, rope, stream);

@@ -30,11 +30,16 @@ def dev(x):
     return torch.from_numpy(np.ascontiguousarray(x)).to(DEV)
 
 
+# bf16: turns of a row from those of one near it, 64 away at most.  The difference to a whole turn is taken in numbers below 128, off by 2^-18, and the
+# frequency is a float, off by 2^-25 of itself, 2^-19 in 64 turns: together 2 pi (2^-18 + 2^-19) of the pair's length
+NEAR = 2 * np.pi * (2.0 ** -18 + 2.0 ** -19)
+
+
 class Problem:
     """Caches of `lens` live retained rows and n_apx approximated rows per sequence in one of three layouts, with junk (NaN blocks
     among it) in every row that is none."""
 
-    def __init__(self, lens, n_apx, H=2, G=4, d=128, dtype="bf16", layout="blocks", room=3, block_rows=16, rope=False, interleaved=False, positions=True, seed=0,
+    def __init__(self, lens, n_apx, H=2, G=4, d=128, dtype="bf16", layout="blocks", room=3, block_rows=16, rope=False, interleaved=False, positions=True, spread=None, seed=0,
                  q_size=1.0, scale=None, caps=None):
         rng = np.random.default_rng(seed)
         self.B, self.H, self.G, self.d, self.dtype, self.layout = len(lens), H, G, d, dtype, layout
@@ -97,6 +102,8 @@ class Problem:
             self.inv_freq = dg.rotary_inv_freq(d, 500000.0)
             offset = 5
             pos = [np.sort(rng.integers(0, 60000, (H, n)), -1).astype(np.int32) if positions else np.tile(np.arange(n, dtype=np.int32), (H, 1)) for n in apx]
+            if spread:
+                pos = [np.stack([spread(rng, n) for _ in range(H)]).astype(np.int32) for n in apx]
             self.pos = [x + offset for x in pos]
             flat = dev(np.concatenate([x.reshape(-1) for x in pos])) if positions and sum(apx) else None
             self.rope, keep = vb.make_rope(self.inv_freq, flat, interleaved, offset)
@@ -137,7 +144,7 @@ class Problem:
                     A = np.abs(self.scale) * (np.abs(k) @ np.abs(q)).max()
                     rel = 2 * (d * U * A + 4 * U * 3 * A * 1.45 + 2 * U) + (2.0 ** -16 if bf16 else 2.0 ** -22) + (n + 2 * d) * U
                     out[b, h * G + g] = p @ v
-                    tol[b, h * G + g] = rel * (p @ size) + (2.0 ** -17 + (2.0 ** -8 if bf16 else 0)) * (p @ turned) + 1e-37
+                    tol[b, h * G + g] = rel * (p @ size) + (2.0 ** -17 + (2.0 ** -8 + NEAR if bf16 else 0)) * (p @ turned) + 1e-37
         return out, tol
 
     def call(self, step=False, out=None, flags=vb.VECTOR_DECODE_OUT_F32, stream=None):
@@ -218,6 +225,26 @@ def test_keys_turned_back(dtype, d, interleaved, positions, G):
     Problem([40, 3], 130, **kw).check()
     Problem([40, 0, 77], [33, 200, 0], layout="sequences", **kw).check(True)
     Problem([40, 3], 0, **kw).check()                    # nothing to turn back
+
+
+SPREADS = {
+    "dense": lambda rng, n: np.sort(rng.choice(4 * n, n, replace=False)),
+    "one in thirty": lambda rng, n: 30 * np.arange(n) + rng.integers(0, 30, n),      # about as far as near goes
+    "jumps": lambda rng, n: np.arange(n) + (np.arange(n) // 37) * 100_000,           # most tiles near, some not
+    "any order": lambda rng, n: rng.permutation(n),
+    "the same": lambda rng, n: np.full(n, 777),
+    "far": lambda rng, n: np.sort(rng.integers(0, 2 ** 24 - 6, n)),
+    "far and dense": lambda rng, n: np.arange(2 ** 24 - 6 - n, 2 ** 24 - 6),
+}
+
+
+@pytest.mark.parametrize("dtype,d", itertools.product(["bf16", "f32"], [64, 128]))
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("spread", SPREADS)
+def test_positions_near_and_far(dtype, d, interleaved, spread):
+    kw = dict(dtype=dtype, d=d, rope=True, interleaved=interleaved, spread=SPREADS[spread])
+    Problem([40, 3], 300, G=4, **kw).check()
+    Problem([5, 0], [77, 260], G=2, layout="sequences", **kw).check(True)
 
 
 @pytest.mark.parametrize("d", [64, 128])
