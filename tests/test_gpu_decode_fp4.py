@@ -247,6 +247,15 @@ def test_positions_near_and_far(dtype, d, interleaved, spread):
     Problem([5, 0], [77, 260], G=2, layout="sequences", **kw).check(True)
 
 
+@pytest.mark.parametrize("dtype,G", [("bf16", 4), ("bf16", 16), ("f32", 3)])
+def test_one_map_for_all_heads(dtype, G):
+    p = Problem([40, 3], 90, H=3, G=G, dtype=dtype)
+    p.W[1:] = p.W[0]
+    p.W_dev = p.W_dev[:1].contiguous()
+    p.cache.W, p.cache.w_shared = p.W_dev.data_ptr(), 1
+    p.check(True)
+
+
 @pytest.mark.parametrize("d", [64, 128])
 def test_many_splits(d):
     """One pair of long segments cut into many pieces, and many pairs."""

@@ -155,3 +155,59 @@ def test_rows_far_into_a_pool():
     want = fo.quantise(wide(x)[0])
     np.testing.assert_array_equal(wide(out), fo.values(*want))
     assert np.array_equal(codes[slots[0]].cpu().numpy(), want[0])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_store_reads_strided_rows(dtype, d):
+    """Tokens first, queries, keys and values of a token side by side."""
+    rng = np.random.default_rng(6)
+    H, T = 3, 41
+    packed = to_dtype(host_rows(rng, (T, 3, H, d)), dtype)
+    shape = vb.Shape(n_q_heads=H, n_kv_heads=H, head_dim=d, seq_len=T, window=1, pool_kernel=1, dtype=vdt(dtype),
+                     k_stride_head=d, k_stride_tok=3 * H * d, v_stride_head=d, v_stride_tok=3 * H * d)
+    slots = rng.permutation(H * T).reshape(H, T)
+    pools = [bytes_full(H * T, d // 2), bytes_full(H * T, d // 32), bytes_full(H * T, d // 2), bytes_full(H * T, d // 32)]
+    vb.vector_store_fp4(shape, packed[:, 1], packed[:, 2], torch.from_numpy(slots).to(DEV), H * T, *pools)
+    torch.cuda.synchronize()
+    for src, codes, scales in ((packed[:, 1], *pools[:2]), (packed[:, 2], *pools[2:])):
+        check_rows(codes.cpu().numpy()[slots], scales.cpu().numpy()[slots], wide(src).transpose(1, 0, 2), "pool")
+
+
+def test_load_to_bf16_is_exact_under_every_scale():
+    codes = torch.arange(32, dtype=torch.uint8, device=DEV).repeat(256, 1) * 8 + 3
+    scales = torch.arange(256, dtype=torch.uint8, device=DEV)[:, None].repeat(1, 2)
+    out = torch.full((256, 64), 7.0, device=DEV, dtype=torch.bfloat16)
+    vb.vector_load_fp4(256, 64, vb.VECTOR_BF16, codes, scales, 256, None, out)
+    torch.cuda.synchronize()
+    with np.errstate(over="ignore"):
+        want = fo.values(codes.cpu().numpy(), scales.cpu().numpy()).astype(np.float32)
+    np.testing.assert_array_equal(out.float().cpu().numpy(), want)
+
+
+def test_as_many_rows_as_a_call_takes():
+    """2^28 tokens (32 GiB of keys), 2^29 rows read back (64 GiB); few of them are somewhere."""
+    d, T, rows = 64, 1 << 28, 100
+    k = torch.zeros(1, T, d, dtype=torch.bfloat16, device=DEV)
+    slots = torch.full((1, T), -1, dtype=torch.int64, device=DEV)
+    some = torch.tensor([0, 31, 12345, (1 << 25) + 7, 1 << 27, T - 33, T - 1], device=DEV)
+    k[0, some] = torch.randn(len(some), d, device=DEV).bfloat16()
+    slots[0, some] = torch.arange(len(some), device=DEV) * 3
+    codes, scales = bytes_full(rows, d // 2), bytes_full(rows, d // 32)
+    shape = vb.Shape(n_q_heads=1, n_kv_heads=1, head_dim=d, seq_len=T, window=1, pool_kernel=1, dtype=vb.VECTOR_BF16)
+    vb.vector_store_fp4(shape, k, None, slots, rows, codes, scales)
+    torch.cuda.synchronize()
+    at = np.arange(len(some)) * 3
+    values = wide(k[0, some])
+    check_rows(codes.cpu().numpy()[at], scales.cpu().numpy()[at], values, "pool")
+    rest = np.setdiff1d(np.arange(rows), at)
+    assert (codes.cpu().numpy()[rest] == 0xA5).all()
+    del k
+    back = torch.full((2, T), -1, dtype=torch.int64, device=DEV)
+    back[1] = slots[0]
+    out = torch.full((2, T, d), 7.0, dtype=torch.bfloat16, device=DEV)
+    vb.vector_load_fp4(2 * T, d, vb.VECTOR_BF16, codes, scales, rows, back, out)
+    torch.cuda.synchronize()
+    np.testing.assert_array_equal(wide(out[1, some]), fo.values(codes.cpu().numpy()[at], scales.cpu().numpy()[at]))
+    out[1, some] = 0
+    assert all(not bool(part.any()) for part in out.view(-1, 1 << 24))
