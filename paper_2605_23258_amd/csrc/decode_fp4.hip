@@ -83,7 +83,8 @@ template <int D> struct Fp4Stage {
   static __device__ __forceinline__ int piece(int row, int piece) { return place(row) * kCode + ((piece ^ twist(place(row))) * 16); }
 };
 // Tiles of a wave: one on its way while one is worked on.  Split launch, us, two stages / three / four (two workgroups per CU) / two and four workgroups:
-// 16 routed sequences of 32768 tokens 18.9 / 19.8 / 21.3 / 21.2, 24 unequal ones 14.0 / 16.1 / 18.3 / 14.7, on rotated keys 20.7 / 22.9 / 33.4 / 28.1,
+// 16 routed sequences of 32768 tokens 18.9 / 19.8 / 21.3 / 21.2, 24 unequal ones 14.0 / 16.1 / 18.3 / 14.7, on rotated keys
+// (before kNearTurns) 20.7 / 22.9 / 33.4 / 28.1,
 // 64 whole ones of 2048 28.3 / 31.1 / 35.0 / 28.0, 16 whole ones of 32768 90.1 / 91.3 / 92.1 / 90.8.
 constexpr int kFp4Stages = 2;
 

@@ -166,9 +166,9 @@ inline bool pick_one_round(const SplitCosts& c, int batch, int n_kv_heads, int c
 
 // Caches held in 4 bits: as many workgroups as run at the same time, per_cu on a CU, cut so that the longest piece is the shortest; steps of 128 rows.
 // What a step of approximated rows takes, in steps of retained ones: they have half the bytes, but as much arithmetic, and sines and cosines
-// where they are turned back.  Split launch, us, these / equal pieces: 24 unequal sequences of up to 16000 tokens on rotated keys 21.2 / 26.4,
-// 16 of 32768 31.4 / 32.1; on plain keys 19.8 / 19.8 (0.6: 19.7), four 11.4 / 11.8 (0.6: 10.2).  More workgroups than run at the same time (1024, 1536)
-// are slower: 16 of 32768 19.8 / 21.5 / 22.4, 24 unequal ones 15.0 / 15.1 / 16.4, on rotated keys 21.2 / 25.1 / 23.6, 64 whole ones of 2048 28.2 / 28.4 / 30.4;
+// where they are turned back.  Split launch, us, these / equal pieces: 24 unequal sequences of up to 16000 tokens on rotated keys 20.3 / 24.0,
+// 16 of 32768 27.4 / 30.3; on plain keys 20.2 / 19.9 (0.6: 21.0), four 10.5 / 11.7 (0.6: 10.8).  More workgroups than run at the same time (1024, 1536)
+// are slower: 16 of 32768 20.2 / 21.0 / 22.2, 24 unequal ones 14.9 / 16.1 / 17.4, on rotated keys 20.3 / 22.8 / 24.8, 64 whole ones of 2048 27.6 / 28.3 / 30.0;
 // the plan of unequal bf16 caches (PlannedSplits), too, since a CU that has done its short pieces leaves the memory to the others: 24
 // unequal ones 17.4 / 18.2, 48 of up to 4000 19.2 / 23.0 (with a ring of three tiles).
 constexpr int kFp4StepRows = 128, kFp4PerCu = 3;
