@@ -182,7 +182,10 @@ __device__ __forceinline__ void attend_fp4(const Fp4Params& f, const RopeParams&
   const uint32_t in_code = in_row * kCode + in_piece * 16;
   const uint8_t* in_scale = (lane < 32 ? k_scales : r_scales) + scale_row * kScale;
   const bool small_blocks = paged && seg.block_shift < 5;
-  bool holes = false;                                  // a block that does not exist has been met
+  // A block that does not exist has been met: from then on a tile's mask of rows is looked at, the one on its way by then included, so
+  // that every stage has one from the start.
+  bool holes = false;
+  if (paged && lane < kFp4Stages) *reinterpret_cast<uint32_t*>(ring + lane * St::kBytes + St::kAlive) = ~0u;
 
   auto fill = [&](int base, unsigned char* st) VEC_INLINE {
     int64_t at_lo = row0 + base, at_hi = at_lo;        // of the tile's first row, less 16 rows of its 17th
@@ -191,7 +194,7 @@ __device__ __forceinline__ void attend_fp4(const Fp4Params& f, const RopeParams&
       if (((base + kFp4TileRows - 1) >> seg.block_shift) - window > kWave - 1) { window = base >> seg.block_shift; load_window(); }
       lo = hi = block_row(base, at_lo);
       at_hi = at_lo;
-      if (seg.block_shift < 5) {
+      if (seg.block_shift < 5 && base + 16 < row_end) {        // (behind the last row there need not be a block)
         hi = block_row(base + 16, at_hi);
         at_hi -= 16;
       }
