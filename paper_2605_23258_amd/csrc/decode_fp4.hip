@@ -286,7 +286,7 @@ __device__ __forceinline__ void attend_fp4(const Fp4Params& f, const RopeParams&
   constexpr int kDims = D / 16;
   const uint32_t to_exponent = 8u * (apart ? kDims / 2 * m / kFp4Block : kDims * m / kFp4Block) + 9u;
   auto exponent = [](uint32_t bytes, uint32_t by) VEC_INLINE { return __uint_as_float(__builtin_amdgcn_alignbit(bytes, bytes, by)); };
-  const uint32_t rest_mask = lo ? 0xffff0000u : 0u;
+  const uint32_t rest_mask = lo ? 0xffff0000u : 0u, rest_half = lo ? 0x8000u : 0u;      // a bf16's bits of a float; half of its last one
   const uint32_t at_dim = m < 8 ? 0x0c0c0706u : 0x07060c0cu;        // kQuad: a weight's leading half in the low or the high half of a word
 
   // a lane's dims always belong to the same kDims / 2 rotary pairs
@@ -370,9 +370,14 @@ __device__ __forceinline__ void attend_fp4(const Fp4Params& f, const RopeParams&
     }
     // kQuad: rows 0 .. 3 and 4 .. 7
     u32x4 weights[kQuad ? 2 : kParts];
+    // A weight in two parts is good to 2^-16 of itself: what the leading eight bits leave is below 2^-7 of it and goes to the nearest of its own
+    // eight bits.  Cutting those off as well is off by up to 2^-15, and always to the same side.
     if constexpr (COLS != 16) {                        // columns of the rest
 #pragma unroll
-      for (int j = 0; j < 8; ++j) w[j] -= __uint_as_float(__float_as_uint(w[j]) & rest_mask);
+      for (int j = 0; j < 8; ++j) {
+        w[j] -= __uint_as_float(__float_as_uint(w[j]) & rest_mask);
+        w[j] = __uint_as_float(__float_as_uint(w[j]) + rest_half);
+      }
     }
     if constexpr (kQuad) {
 #pragma unroll
@@ -383,7 +388,8 @@ __device__ __forceinline__ void attend_fp4(const Fp4Params& f, const RopeParams&
 #pragma unroll
       for (int part = 0; part < kParts; ++part) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) weights[part][i] = high_halves(w[2 * i], w[2 * i + 1]);
+        for (int i = 0; i < 4; ++i)
+          weights[part][i] = part > 0 && part + 1 == kParts ? pack_bf16(w[2 * i], w[2 * i + 1]) : high_halves(w[2 * i], w[2 * i + 1]);
         if (part + 1 < kParts) {
 #pragma unroll
           for (int j = 0; j < 8; ++j) w[j] -= leading(w[j]);
