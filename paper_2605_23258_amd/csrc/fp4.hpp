@@ -18,8 +18,6 @@ typedef __attribute__((ext_vector_type(2))) float f32x2;
 typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 typedef __attribute__((ext_vector_type(8))) int i32x8;
 typedef __attribute__((ext_vector_type(2))) short s16x2;
-typedef __attribute__((ext_vector_type(4), aligned(4))) uint32_t u32x4_a4;   // scales of rows at any row
-typedef __attribute__((ext_vector_type(4), aligned(2))) uint32_t u32x4_a2;
 
 // f(0), f(1), .. with the number as a constant, which the conversions' byte selectors have to be
 template <typename F, int... I> __device__ __forceinline__ void for_constants(std::integer_sequence<int, I...>, F f) {
