@@ -421,7 +421,8 @@ typedef struct {
   int32_t reserved;
   const int32_t* len_held;       /* device [batch], or NULL: no request holds blocks yet     */
   const int32_t* len;            /* device [batch]                                           */
-  const int32_t* free_blocks;    /* device [n_free]: ids of free blocks; NULL: 0, 1, 2, ..   */
+  const int32_t* free_blocks;    /* device [n_free]: ids of free blocks; NULL: 0, 1, 2, ..  It is only read: the blocks of
+                                    requests that have ended are for the caller to put into the list of a later call */
   const int32_t* n_used;         /* device [1], or NULL: as many of them, from the front, have been taken by calls before (0); add
                                     counts[0] to it on the GPU, and no length or count ever has to come to the host */
 } vector_blocks;
@@ -465,7 +466,8 @@ VECTOR_API int vector_load_fp4(int64_t n_rows, int32_t head_dim, int32_t dtype, 
 
 /* vector_cache with its rows in 4 bits.  Everything is laid out as there, in rows of codes and rows of scales: k_ret, k_ret_scale
  * [batch, Hkv, cap_retain, ..] and so on; dtype is that of q, W, out and the step's token.
- * cap_retain and n_approx, and those of every sequence: up to 2^30 (VECTOR_ERR_SHAPE beyond). */
+ * cap_retain and n_approx: up to 2^30 (VECTOR_ERR_SHAPE beyond).  Those of the sequences may not be more either; they lie on the device, like
+ * the sequences' first rows, and no call looks at them before it uses them. */
 typedef struct {
   int32_t batch, n_q_heads, n_kv_heads, head_dim;
   int32_t dtype;
@@ -487,15 +489,17 @@ typedef struct {
   int32_t ret_block_rows;
   int32_t ret_blocks_per_seq;
   int32_t n_blocks;              /* paged: blocks of the pools.  Rows of a block whose id is not in 0 .. n_blocks - 1 are no rows: they
-                                    take no part, and a step's token in one is attended but not stored */
+                                    take no part, and a step's token in one is attended but not stored.  len_retain counts it
+                                    all the same: it is the len_live of vector_block_tables that leaves out what has no block */
   int32_t reserved;
 } vector_cache_fp4;
 
 /* vector_decode_attn and vector_decode_step over a cache in 4 bits, rope NULL, or vector_decode_attn_rope and
  * vector_decode_step_rope.  Same arguments, flags (VECTOR_DECODE_OUT_F32), outputs and errors.  The step rounds the new token to 4 bits
  * and attends to it as it lies in the cache from then on, so that it gives what storing the row and
- * vector_decode_attn_fp4 would.  The products run on the matrix cores in bf16 with fp32 sums; bf16: weights to 2^-16 relative at least;
- * fp32: query and weights with all their bits.  VECTOR_DECODE_LITERAL: VECTOR_ERR_DTYPE.
+ * vector_decode_attn_fp4 would.  The products run on the matrix cores in bf16 with fp32 sums; bf16: weights to 2^-16 relative at least,
+ * keys that are turned back rounded to bf16 once more, as those of a bf16 cache are; fp32: query, weights and keys turned back in as many parts as hold their
+ * bits.  VECTOR_DECODE_LITERAL: VECTOR_ERR_DTYPE.
  * ws: vector_decode_fp4_workspace_bytes(cache) bytes (0 for a shape that is refused), 256-byte aligned. */
 VECTOR_API size_t vector_decode_fp4_workspace_bytes(const vector_cache_fp4* cache);
 VECTOR_API int vector_decode_attn_fp4(const vector_cache_fp4* cache, const vector_rope* rope, const void* q, float scale, void* out,
