@@ -170,7 +170,8 @@ inline bool pick_one_round(const SplitCosts& c, int batch, int n_kv_heads, int c
 // 16 of 32768 27.4 / 30.3; on plain keys 20.2 / 19.9 (0.6: 21.0), four 10.5 / 11.7 (0.6: 10.8).  More workgroups than run at the same time (1024, 1536)
 // are slower: 16 of 32768 20.2 / 21.0 / 22.2, 24 unequal ones 14.9 / 16.1 / 17.4, on rotated keys 20.3 / 22.8 / 24.8, 64 whole ones of 2048 27.6 / 28.3 / 30.0;
 // the plan of unequal bf16 caches (PlannedSplits), too, since a CU that has done its short pieces leaves the memory to the others: 24
-// unequal ones 17.4 / 18.2, 48 of up to 4000 19.2 / 23.0 (with a ring of three tiles).
+// unequal ones 17.4 / 18.2, 48 of up to 4000 19.2 / 23.0 (with a ring of three tiles).  On rotated keys the plan was ahead of equal pieces, 24.3 / 25.9; it has not been measured
+// against these.
 constexpr int kFp4StepRows = 128, kFp4PerCu = 3;
 constexpr double kFp4Approx = 0.8, kFp4Turned = 2.5;
 inline void pick_splits_fp4(int batch, int n_kv_heads, int cap_retain, int n_approx, double apx_cost, int per_cu, int& s_ret, int& s_apx) {
