@@ -371,7 +371,8 @@ __device__ __forceinline__ void attend_fp4(const Fp4Params& f, const RopeParams&
     // kQuad: rows 0 .. 3 and 4 .. 7
     u32x4 weights[kQuad ? 2 : kParts];
     // A weight in two parts is good to 2^-16 of itself: what the leading eight bits leave is below 2^-7 of it and goes to the nearest of its own
-    // eight bits.  Cutting those off as well is off by up to 2^-15, and always to the same side.
+    // eight bits.  Cutting those off as well is off by up to 2^-15, and always to the same side.  Split launch, us, cut / rounded: 16 whole sequences of 32768
+    // tokens 89.8 / 90.4, 24 unequal ones on rotated keys 20.7 / 20.3, 16 of 16384 at 64 dims 29.3 / 30.0, with sixteen query heads 51.8 / 50.6.
     if constexpr (COLS != 16) {                        // columns of the rest
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
